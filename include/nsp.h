@@ -306,6 +306,81 @@ int nsp_a2a_gather_heads(const void* src, void* dst, int64_t tokens, int32_t hea
 int nsp_a2a_scatter_heads(const void* src, void* dst, int64_t tokens, int32_t heads, int32_t heads_per_block,
                           int32_t n_blocks, int32_t head_dim, int32_t dtype, const int32_t* first_head, void* stream);
 
+/*
+ * Rotary positions of queries and keys, and the way back of their gradients: a step of a layer between the projections and
+ * the attention (on a GPU's token slices in front of the all-to-all, or on the packed tensors the attention reads).
+ * The first rot_dim elements of a head are rot_dim / 2 pairs, pair i of NSP_ROPE_HALF the elements (i, rot_dim / 2 + i), of
+ * NSP_ROPE_INTERLEAVED (2 i, 2 i + 1). At position p a pair (a, b) becomes (a c - b s, b c + a s) with
+ * c = magnitude * cos(p * inv_freq[i]), s = magnitude * sin(p * inv_freq[i]); inverse != 0: with -s, the gradient of that. The
+ * other elements pass as they are. fp32 arithmetic, angles exact for any position (64-bit fixed point), one rounding.
+ *
+ * tensors: host array [n_tensors], n_tensors <= NSP_ROPE_MAX_TENSORS, all of them in one launch: for example q and k of a node,
+ * or of every node of a chain. A tensor is [tokens, heads, head_dim] with element strides between tokens and heads
+ * (0 .. 2^31; the elements of a head are contiguous), of its own type. positions: DEVICE int64 [tokens], any values, or NULL for
+ * 0, 1, 2, ... y may be x with the same strides (in place); otherwise the tensors of a call do not overlap one another. Rows of a
+ * y must not overlap. Addresses and strides that are multiples of 16 bytes are fastest; any that fit the type will do.
+ * inv_freq: HOST [rot_dim / 2], radians per position, finite; it is read by the call itself (a captured call keeps its values).
+ * Errors: INVALID_ARG, UNSUPPORTED (more than NSP_ROPE_MAX_TENSORS tensors, rot_dim > NSP_ROPE_MAX_ROT, head_dim >
+ * NSP_ROPE_MAX_HEAD_DIM, more than 65536 heads, 2^31 or more heads of all tokens of a tensor), CUDA.
+ *
+ * nsp_rope_frequencies fills inv_freq [rot_dim / 2] and *magnitude (both host): base^(-2 i / rot_dim), for contexts longer than
+ * the trained ones scaled by scaling->kind (scaling may be NULL: NSP_ROPE_PLAIN):
+ *   NSP_ROPE_LINEAR  every frequency divided by scale
+ *   NSP_ROPE_BASE    base multiplied by scale^(rot_dim / (rot_dim - 2)): the last pair's frequency divided by scale, the first left
+ *   NSP_ROPE_PARTS   pairs that make more than fast_turns turns within trained_tokens left, those with fewer than slow_turns
+ *                    divided by scale, a linear ramp over the pairs in between; magnitude = 0.1 ln(scale) + 1 (1 otherwise)
+ * Host only. Errors: INVALID_ARG (rot_dim odd or outside 2 .. NSP_ROPE_MAX_ROT, base <= 1, scale < 1, not fast_turns > slow_turns > 0,
+ * trained_tokens <= 0).
+ */
+#define NSP_ROPE_MAX_TENSORS 64
+#define NSP_ROPE_MAX_ROT 512
+#define NSP_ROPE_MAX_HEAD_DIM 1024
+enum { NSP_ROPE_HALF = 0, NSP_ROPE_INTERLEAVED = 1 };
+enum { NSP_ROPE_PLAIN = 0, NSP_ROPE_LINEAR = 1, NSP_ROPE_BASE = 2, NSP_ROPE_PARTS = 3 };
+typedef struct {
+  const void* x;
+  void* y;
+  const int64_t* positions;
+  int64_t tokens, x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+  int32_t heads, dtype;
+} nsp_rope_tensor_t;
+typedef struct {
+  int32_t kind;
+  double scale, trained_tokens, fast_turns, slow_turns;
+} nsp_rope_scaling_t;
+int nsp_rope_frequencies(int32_t rot_dim, double base, const nsp_rope_scaling_t* scaling, double* inv_freq, float* magnitude);
+int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int32_t head_dim, int32_t rot_dim, int32_t layout,
+             const double* inv_freq, float magnitude, int32_t inverse, void* stream);
+
+/*
+ * Layer norm (NSP_NORM_LAYER) and RMS norm (NSP_NORM_RMS) over the last axis, forward and backward: of hidden states, or of
+ * queries and keys head by head.
+ *   forward   mean = sum(x) / dim (RMS: 0), rstd = (sum((x - mean)^2) / dim + eps)^(-1/2), y = (x - mean) rstd weight + bias
+ *   backward  h = (x - mean) rstd, t = dy weight, dx = rstd (t - h mean(t h) - mean(t)) (RMS: without mean(t)),
+ *             dweight = sum over the rows of dy h, dbias = sum of dy
+ * x, y, dy, dx are rows [outer, inner, dim] of dtype with element strides (0 .. 2^31) of the outer two axes (rows of a matrix:
+ * inner = 1); weight, bias [dim] of w_dtype, NULL = 1 and 0; mean, rstd fp32 [outer * inner], written by the forward pass where
+ * they are not NULL and read by the backward pass (RMS: mean is not read). dweight, dbias fp32 [dim], overwritten, either may be
+ * NULL (not wanted). All sums are in fp32; dweight and dbias are added up in a fixed order (the same bits in every run). y may be
+ * x, and dx may be x or dy, with the same strides; otherwise outputs overlap nothing. Rows of outputs must not overlap. Addresses
+ * and strides that are multiples of 16 bytes and dim a multiple of 8 are fastest; any that fit the types will do.
+ * ws: at least nsp_norm_bwd_ws_bytes(outer * inner, dim), 16-byte aligned, where dweight or dbias is wanted; contents undefined
+ * afterwards, and not shared by calls that may overlap.
+ * Errors: INVALID_ARG, UNSUPPORTED (dim > NSP_NORM_MAX_DIM, 2^31 or more rows), WORKSPACE, CUDA.
+ */
+#define NSP_NORM_MAX_DIM 16384
+enum { NSP_NORM_LAYER = 0, NSP_NORM_RMS = 1 };
+typedef struct {
+  const void* data;
+  int64_t outer_stride, inner_stride;
+} nsp_rows_t;
+int nsp_norm_fwd(const nsp_rows_t* x, const void* weight, const void* bias, const nsp_rows_t* y, float* mean, float* rstd, int64_t outer,
+                 int32_t inner, int32_t dim, int32_t dtype, int32_t w_dtype, int32_t kind, float eps, void* stream);
+int nsp_norm_bwd_ws_bytes(int64_t rows, int32_t dim, size_t* bytes);
+int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const void* weight, const float* mean, const float* rstd, const nsp_rows_t* dx,
+                 float* dweight, float* dbias, int64_t outer, int32_t inner, int32_t dim, int32_t dtype, int32_t w_dtype, int32_t kind,
+                 void* ws, size_t ws_bytes, void* stream);
+
 /* Read the device status record {code, item, where, aux}; code 0 = healthy. Synchronises the device. */
 int nsp_device_status(const nsp_plan_t* plan, int32_t out[4]);
 

@@ -25,6 +25,11 @@ NSP_F32 = 1
 NSP_MAX_RUNS = 32
 NSP_PLAN_DETERMINISTIC_DQ = 1
 NSP_PLAN_ROUNDED_DQ = 2
+NSP_ROPE_HALF, NSP_ROPE_INTERLEAVED = 0, 1
+NSP_ROPE_PLAIN, NSP_ROPE_LINEAR, NSP_ROPE_BASE, NSP_ROPE_PARTS = 0, 1, 2, 3
+NSP_ROPE_MAX_TENSORS, NSP_ROPE_MAX_ROT, NSP_ROPE_MAX_HEAD_DIM = 64, 512, 1024
+NSP_NORM_LAYER, NSP_NORM_RMS = 0, 1
+NSP_NORM_MAX_DIM = 16384
 
 EXPORTS = [
     "nsp_plan_tiles", "nsp_plan_sizes", "nsp_plan_get", "nsp_attn_fwd", "nsp_attn_bwd", "nsp_device_status",
@@ -33,6 +38,7 @@ EXPORTS = [
     "nsp_cost_table", "nsp_route_sp_tree", "nsp_a2a_gather_heads", "nsp_a2a_scatter_heads",
     "nsp_selftest_wait_timeout", "nsp_a2a_gather_heads_to", "nsp_plan_set_wait_limit",
     "nsp_plan_step_host_ws_bytes", "nsp_attn_step_host", "nsp_trim", "nsp_plan_pair_items",
+    "nsp_rope_frequencies", "nsp_rope", "nsp_norm_fwd", "nsp_norm_bwd_ws_bytes", "nsp_norm_bwd",
 ]
 CHECKED_EXPORTS = ["nsp_checked_withhold_load", "nsp_checked_withhold_pair_load"]  # libnsp_checked.so only
 NSP_COST_BUCKETS = 16
@@ -56,6 +62,21 @@ class NspError(RuntimeError):
 class PlanOpts(ctypes.Structure):
     _fields_ = [("bm", ctypes.c_int32), ("bn", ctypes.c_int32), ("order_version", ctypes.c_int32),
                 ("flags", ctypes.c_int32)]
+
+
+class RopeTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("tokens", ctypes.c_int64),
+                ("x_token_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64), ("y_token_stride", ctypes.c_int64),
+                ("y_head_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("scale", ctypes.c_double), ("trained_tokens", ctypes.c_double),
+                ("fast_turns", ctypes.c_double), ("slow_turns", ctypes.c_double)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("outer_stride", ctypes.c_int64), ("inner_stride", ctypes.c_int64)]
 
 
 def lib() -> ctypes.CDLL:
@@ -109,6 +130,17 @@ def lib() -> ctypes.CDLL:
         L.nsp_attn_step_host.restype = ctypes.c_int
         L.nsp_plan_set_wait_limit.argtypes = [vp, ctypes.c_int64]
         L.nsp_plan_set_wait_limit.restype = ctypes.c_int
+        L.nsp_rope_frequencies.argtypes = [ctypes.c_int32, ctypes.c_double, ctypes.POINTER(RopeScaling), vp,
+                                           ctypes.POINTER(ctypes.c_float)]
+        L.nsp_rope.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_float,
+                               ctypes.c_int32, vp]
+        rows = ctypes.POINTER(Rows)
+        L.nsp_norm_fwd.argtypes = [rows, vp, vp, rows, vp, vp, ctypes.c_int64] + [ctypes.c_int32] * 5 + [ctypes.c_float, vp]
+        L.nsp_norm_bwd_ws_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+        L.nsp_norm_bwd.argtypes = [rows, rows, vp, vp, vp, rows, vp, vp, ctypes.c_int64] + [ctypes.c_int32] * 5 + [
+            vp, ctypes.c_size_t, vp]
+        for f in (L.nsp_rope_frequencies, L.nsp_rope, L.nsp_norm_fwd, L.nsp_norm_bwd_ws_bytes, L.nsp_norm_bwd):
+            f.restype = ctypes.c_int
         if hasattr(L, "nsp_checked_withhold_load"):
             L.nsp_checked_withhold_load.argtypes = [vp, ctypes.c_int]
             L.nsp_checked_withhold_load.restype = ctypes.c_int
@@ -570,3 +602,172 @@ def nsp_attn_bwd_static(plan: Plan, q, k, v, o, d_o, lse, dq, dk, dv, softmax_sc
                                    _ptr(dk), _ptr(dv), dq_dtype, dkv_dtype, float(softmax_scale), _stream_ptr(stream))
     if rc != NSP_OK:
         raise NspError(rc, "nsp_attn_bwd_static")
+
+
+# ---- token-wise operators around the attention
+def _refuse(what, why, code=NSP_ERR_INVALID_ARG):
+    raise NspError(code, f"{what}: {why}")
+
+
+def _on_device(what, named, here):
+    """Refuse tensors that are not on the current device. named: (name, tensor) pairs; None is left out."""
+    import torch
+
+    for name, t in named:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            _refuse(what, f"{name} must be a CUDA tensor")
+        if t.get_device() != here:
+            _refuse(what, f"{name} is on {t.device}, not on the current device")
+
+
+def _dtype_of(what, name, t):
+    import torch
+
+    if t.dtype == torch.bfloat16:
+        return NSP_BF16
+    if t.dtype == torch.float32:
+        return NSP_F32
+    _refuse(what, f"{name} has dtype {t.dtype}")
+
+
+def nsp_rope_frequencies(rot_dim, base=10000.0, kind=NSP_ROPE_PLAIN, scale=1.0, trained_tokens=0.0, fast_turns=32.0,
+                         slow_turns=1.0):
+    """(radians per position float64 [rot_dim / 2], magnitude) of rotary positions (host only); kind: NSP_ROPE_PLAIN, or how
+    they are scaled for contexts `scale` times the trained ones (see nsp.h)."""
+    out = np.zeros(max(int(rot_dim) // 2, 1), np.float64)
+    m = ctypes.c_float()
+    sc = RopeScaling(int(kind), float(scale), float(trained_tokens), float(fast_turns), float(slow_turns))
+    rc = lib().nsp_rope_frequencies(int(rot_dim), float(base), ctypes.byref(sc), _ptr(out), ctypes.byref(m))
+    if rc != NSP_OK:
+        raise NspError(rc, "nsp_rope_frequencies")
+    return out, float(m.value)
+
+
+def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, inverse=False, stream=None):
+    """Rotate the heads of xs (a tensor [tokens, heads, head_dim], or a list of them with one head_dim) by their positions into
+    ys (of the same shapes and types; x itself: in place), all in one launch. positions: int64 CUDA tensor [tokens], a list of
+    them, or None (0, 1, 2, ...). inv_freq: float64 [rot_dim / 2] on the host. inverse: the gradient's way back."""
+    import torch
+
+    what = "nsp_rope"
+    if isinstance(xs, torch.Tensor):
+        xs, ys = [xs], [ys]
+    if not isinstance(positions, (list, tuple)):
+        positions = [positions] * len(xs)
+    if len(ys) != len(xs) or len(positions) != len(xs):
+        _refuse(what, "as many outputs and positions as inputs")
+    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if freq.ndim != 1 or len(freq) == 0:
+        _refuse(what, "inv_freq holds one frequency per rotated pair")
+    if not xs:
+        return
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    array = (RopeTensor * len(xs))()
+    head_dim = xs[0].shape[-1] if isinstance(xs[0], torch.Tensor) and xs[0].dim() == 3 else 0
+    for a, x, y, pos in zip(array, xs, ys, positions):
+        _on_device(what, (("x", x), ("y", y), ("positions", pos)), here)
+        if x.dim() != 3 or x.shape[2] != head_dim or y.shape != x.shape or y.dtype != x.dtype:
+            _refuse(what, "x and y are [tokens, heads, head_dim] of one shape and type, with one head_dim in all")
+        if head_dim > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+            _refuse(what, "the elements of a head must be contiguous")
+        if pos is not None and (pos.dtype != torch.int64 or pos.dim() != 1 or not pos.is_contiguous() or pos.numel() != x.shape[0]):
+            _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
+        a.dtype = _dtype_of(what, "x", x)
+        if x.numel() == 0:
+            a.heads = max(x.shape[1], 1)  # tokens = 0: nothing to do
+            continue
+        a.x, a.y, a.positions = x.data_ptr(), y.data_ptr(), None if pos is None else pos.data_ptr()
+        a.tokens, a.heads = x.shape[0], x.shape[1]
+        a.x_token_stride, a.x_head_stride = x.stride(0), x.stride(1)
+        a.y_token_stride, a.y_head_stride = y.stride(0), y.stride(1)
+    rc = lib().nsp_rope(array, len(xs), head_dim, 2 * len(freq), int(layout), _ptr(freq), float(magnitude), int(bool(inverse)),
+                        _stream_ptr(stream))
+    if rc != NSP_OK:
+        raise NspError(rc, what)
+
+
+def _rows(what, name, t, like=None):
+    """(Rows, outer, inner, dim) of a tensor [rows, dim] or [outer, inner, dim] with contiguous last axis."""
+    if t.dim() not in (2, 3) or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
+        _refuse(what, f"{name} must be [rows, dim] or [outer, inner, dim]" + (", of x's shape and type" if like is not None else ""))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        _refuse(what, f"the last axis of {name} must be contiguous")
+    three = t.dim() == 3
+    return (Rows(t.data_ptr() or None, t.stride(0), t.stride(1) if three else 0), t.shape[0], t.shape[1] if three else 1, t.shape[-1])
+
+
+def _norm_vectors(what, named, dim, dtypes):
+    for name, t in named:
+        if t is not None and (t.numel() != dim or not t.is_contiguous() or t.dtype not in dtypes):
+            _refuse(what, f"{name} must be contiguous, with {dim} elements of {dtypes}")
+
+
+def _norm_stats(what, named, rows):
+    import torch
+
+    for name, t in named:
+        if t is not None and (t.numel() != rows or not t.is_contiguous() or t.dtype != torch.float32):
+            _refuse(what, f"{name} must be a contiguous float32 tensor with one entry per row ({rows})")
+
+
+def nsp_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NSP_NORM_LAYER, stream=None):
+    """Layer norm or RMS norm of the rows of x [rows, dim] or [outer, inner, dim] into y (x itself: in place). weight, bias [dim]
+    (bf16 or fp32, None = 1 and 0); mean, rstd: fp32, one entry per row, for the backward pass (None: not wanted)."""
+    import torch
+
+    what = "nsp_norm_fwd"
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    _on_device(what, (("x", x), ("y", y), ("weight", weight), ("bias", bias), ("mean", mean), ("rstd", rstd)), here)
+    rx, outer, inner, dim = _rows(what, "x", x)
+    ry = _rows(what, "y", y, x)[0]
+    _norm_vectors(what, (("weight", weight), ("bias", bias)), dim, (torch.bfloat16, torch.float32))
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        _refuse(what, "weight and bias have one type")
+    _norm_stats(what, (("mean", mean), ("rstd", rstd)), outer * inner)
+    dtype = _dtype_of(what, "x", x)
+    if outer * inner == 0 or dim == 0:
+        return
+    one = weight if weight is not None else bias
+    rc = lib().nsp_norm_fwd(ctypes.byref(rx), _ptr(weight), _ptr(bias), ctypes.byref(ry), _ptr(mean), _ptr(rstd), outer, inner, dim, dtype,
+                            NSP_F32 if one is None else _dtype_of(what, "weight", one), int(kind), float(eps), _stream_ptr(stream))
+    if rc != NSP_OK:
+        raise NspError(rc, what)
+
+
+def nsp_norm_bwd_ws_bytes(rows, dim) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().nsp_norm_bwd_ws_bytes(int(rows), int(dim), ctypes.byref(n))
+    if rc != NSP_OK:
+        raise NspError(rc, "nsp_norm_bwd_ws_bytes")
+    return int(n.value)
+
+
+def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NORM_LAYER, stream=None):
+    """Backward pass of nsp_norm_fwd: dx of x's shape and type (x or dy itself: in place), dweight and dbias fp32 [dim]
+    (overwritten; None: not wanted). ws: a CUDA tensor of at least nsp_norm_bwd_ws_bytes(rows, dim) bytes (None where neither
+    is wanted)."""
+    import torch
+
+    what = "nsp_norm_bwd"
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    _on_device(what, (("x", x), ("dy", dy), ("dx", dx), ("weight", weight), ("mean", mean), ("rstd", rstd), ("dweight", dweight),
+                      ("dbias", dbias), ("ws", ws)), here)
+    rx, outer, inner, dim = _rows(what, "x", x)
+    rdy, rdx = _rows(what, "dy", dy, x)[0], _rows(what, "dx", dx, x)[0]
+    _norm_vectors(what, (("weight", weight),), dim, (torch.bfloat16, torch.float32))
+    _norm_vectors(what, (("dweight", dweight), ("dbias", dbias)), dim, (torch.float32,))
+    _norm_stats(what, (("mean", mean), ("rstd", rstd)), outer * inner)
+    if rstd is None or (mean is None and kind == NSP_NORM_LAYER):
+        _refuse(what, "the forward pass's statistics are needed")
+    _check_ws(what, ws)
+    dtype = _dtype_of(what, "x", x)
+    if dim == 0:
+        return
+    rc = lib().nsp_norm_bwd(ctypes.byref(rx), ctypes.byref(rdy), _ptr(weight), _ptr(mean), _ptr(rstd), ctypes.byref(rdx), _ptr(dweight),
+                            _ptr(dbias), outer, inner if outer * inner else 1, dim, dtype,
+                            NSP_F32 if weight is None else _dtype_of(what, "weight", weight), int(kind), _ptr(ws),
+                            0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream))
+    if rc != NSP_OK:
+        raise NspError(rc, what)
