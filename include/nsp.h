@@ -381,6 +381,39 @@ int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const void* weight, 
                  float* dweight, float* dbias, int64_t outer, int32_t inner, int32_t dim, int32_t dtype, int32_t w_dtype, int32_t kind,
                  void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * The gated half of a feed-forward block: both projections, the activation and the product, forward and backward.
+ *   forward   g = x w_gate^T, u = x w_up^T, h = act(g) u
+ *   backward  dg = dh u act'(g), du = dh act(g); dw_gate = dg^T x, dw_up = du^T x, dx = dg w_gate + du w_up
+ * act: NSP_ACT_SILU (x / (1 + e^-x)) or NSP_ACT_GELU (x times the normal distribution function, by erf).
+ * x, dx [rows, d_model]; w_gate, w_up, dw_gate, dw_up [d_ff, d_model]; h, dh, g, u [rows, d_ff]: bf16 matrices with element
+ * strides between rows (at least the row's length, multiples of 8) and 16-byte aligned addresses; d_model and d_ff multiples of 8.
+ * The forward pass writes g and u for the backward pass where they are not NULL. Products accumulate in fp32; h is formed from
+ * the fp32 accumulators; dg and du, operands of products, are rounded to bf16 in the workspace; every output is rounded once.
+ * The gradients are overwritten; dx may be NULL (not wanted), and so may dw_gate and dw_up together. Outputs overlap nothing else.
+ * ws: at least nsp_glu_bwd_ws_bytes(rows, d_model, d_ff), 256-byte aligned; contents undefined afterwards, and not shared by calls
+ * that may overlap. The results are the same bits in every run.
+ * Errors: INVALID_ARG, UNSUPPORTED (d_model or d_ff not a multiple of 8 or above NSP_GLU_MAX_DIM, rows * d_ff >= 2^34, a device
+ * other than sm_100), WORKSPACE, CUDA, DEVICE_TIMEOUT.
+ *
+ * The kernels of these calls belong to no plan: a device-side wait that runs out (about two seconds) is recorded once per device,
+ * every later nsp_glu call on it answers with DEVICE_TIMEOUT, and nsp_glu_status synchronises the current device and reads the
+ * record {code, tile, where, aux}; code 0 = healthy. The first call on a device looks it up and allocates 16 bytes of host memory.
+ */
+#define NSP_GLU_MAX_DIM 1048576
+enum { NSP_ACT_SILU = 0, NSP_ACT_GELU = 1 };
+typedef struct {
+  const void* data;
+  int64_t row_stride;
+} nsp_matrix_t;
+int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, const nsp_matrix_t* w_up, const nsp_matrix_t* h, const nsp_matrix_t* g,
+                const nsp_matrix_t* u, int64_t rows, int32_t d_model, int32_t d_ff, int32_t act, void* stream);
+int nsp_glu_bwd_ws_bytes(int64_t rows, int32_t d_model, int32_t d_ff, size_t* bytes);
+int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const nsp_matrix_t* w_gate, const nsp_matrix_t* w_up, const nsp_matrix_t* g,
+                const nsp_matrix_t* u, const nsp_matrix_t* dx, const nsp_matrix_t* dw_gate, const nsp_matrix_t* dw_up, int64_t rows,
+                int32_t d_model, int32_t d_ff, int32_t act, void* ws, size_t ws_bytes, void* stream);
+int nsp_glu_status(int32_t out[4]);
+
 /* Read the device status record {code, item, where, aux}; code 0 = healthy. Synchronises the device. */
 int nsp_device_status(const nsp_plan_t* plan, int32_t out[4]);
 

@@ -30,6 +30,8 @@ NSP_ROPE_PLAIN, NSP_ROPE_LINEAR, NSP_ROPE_BASE, NSP_ROPE_PARTS = 0, 1, 2, 3
 NSP_ROPE_MAX_TENSORS, NSP_ROPE_MAX_ROT, NSP_ROPE_MAX_HEAD_DIM = 64, 512, 1024
 NSP_NORM_LAYER, NSP_NORM_RMS = 0, 1
 NSP_NORM_MAX_DIM = 16384
+NSP_ACT_SILU, NSP_ACT_GELU = 0, 1
+NSP_GLU_MAX_DIM = 1048576
 
 EXPORTS = [
     "nsp_plan_tiles", "nsp_plan_sizes", "nsp_plan_get", "nsp_attn_fwd", "nsp_attn_bwd", "nsp_device_status",
@@ -39,6 +41,7 @@ EXPORTS = [
     "nsp_selftest_wait_timeout", "nsp_a2a_gather_heads_to", "nsp_plan_set_wait_limit",
     "nsp_plan_step_host_ws_bytes", "nsp_attn_step_host", "nsp_trim", "nsp_plan_pair_items",
     "nsp_rope_frequencies", "nsp_rope", "nsp_norm_fwd", "nsp_norm_bwd_ws_bytes", "nsp_norm_bwd",
+    "nsp_glu_fwd", "nsp_glu_bwd_ws_bytes", "nsp_glu_bwd", "nsp_glu_status",
 ]
 CHECKED_EXPORTS = ["nsp_checked_withhold_load", "nsp_checked_withhold_pair_load"]  # libnsp_checked.so only
 NSP_COST_BUCKETS = 16
@@ -77,6 +80,10 @@ class RopeScaling(ctypes.Structure):
 
 class Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("outer_stride", ctypes.c_int64), ("inner_stride", ctypes.c_int64)]
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
 
 
 def lib() -> ctypes.CDLL:
@@ -139,6 +146,13 @@ def lib() -> ctypes.CDLL:
         L.nsp_norm_bwd_ws_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
         L.nsp_norm_bwd.argtypes = [rows, rows, vp, vp, vp, rows, vp, vp, ctypes.c_int64] + [ctypes.c_int32] * 5 + [
             vp, ctypes.c_size_t, vp]
+        matrix = ctypes.POINTER(Matrix)
+        L.nsp_glu_fwd.argtypes = [matrix] * 6 + [ctypes.c_int64] + [ctypes.c_int32] * 3 + [vp]
+        L.nsp_glu_bwd_ws_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+        L.nsp_glu_bwd.argtypes = [matrix] * 9 + [ctypes.c_int64] + [ctypes.c_int32] * 3 + [vp, ctypes.c_size_t, vp]
+        L.nsp_glu_status.argtypes = [i32p]
+        for f in (L.nsp_glu_fwd, L.nsp_glu_bwd_ws_bytes, L.nsp_glu_bwd, L.nsp_glu_status):
+            f.restype = ctypes.c_int
         for f in (L.nsp_rope_frequencies, L.nsp_rope, L.nsp_norm_fwd, L.nsp_norm_bwd_ws_bytes, L.nsp_norm_bwd):
             f.restype = ctypes.c_int
         if hasattr(L, "nsp_checked_withhold_load"):
@@ -771,3 +785,74 @@ def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NOR
                             0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
+
+
+def _matrix(what, name, t, rows, cols):
+    """Matrix of a bf16 tensor [rows, cols] with contiguous rows (None: a null pointer)."""
+    import torch
+
+    if t is None:
+        return None
+    if t.dtype != torch.bfloat16:
+        _refuse(what, f"{name} has dtype {t.dtype}")
+    if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        _refuse(what, f"{name} must be [{rows}, {cols}] with contiguous rows")
+    return ctypes.byref(Matrix(t.data_ptr() or None, t.stride(0)))
+
+
+def _glu_sizes(what, x, w_gate):
+    if x.dim() != 2 or w_gate.dim() != 2:
+        _refuse(what, "x is [rows, d_model], w_gate and w_up are [d_ff, d_model]")
+    return x.shape[0], x.shape[1], w_gate.shape[0]
+
+
+def nsp_glu_fwd(x, w_gate, w_up, h, g=None, u=None, act=NSP_ACT_SILU, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T), bf16 tensors x [rows, d_model], w_gate and w_up [d_ff, d_model], h [rows, d_ff]; g and u
+    (as h): the two projections, for the backward pass."""
+    import torch
+
+    what = "nsp_glu_fwd"
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    _on_device(what, (("x", x), ("w_gate", w_gate), ("w_up", w_up), ("h", h), ("g", g), ("u", u)), here)
+    rows, d, f = _glu_sizes(what, x, w_gate)
+    rc = lib().nsp_glu_fwd(_matrix(what, "x", x, rows, d), _matrix(what, "w_gate", w_gate, f, d), _matrix(what, "w_up", w_up, f, d),
+                           _matrix(what, "h", h, rows, f), _matrix(what, "g", g, rows, f), _matrix(what, "u", u, rows, f), rows, d, f,
+                           int(act), _stream_ptr(stream))
+    if rc != NSP_OK:
+        raise NspError(rc, what)
+
+
+def nsp_glu_bwd_ws_bytes(rows, d_model, d_ff) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().nsp_glu_bwd_ws_bytes(int(rows), int(d_model), int(d_ff), ctypes.byref(n))
+    if rc != NSP_OK:
+        raise NspError(rc, "nsp_glu_bwd_ws_bytes")
+    return int(n.value)
+
+
+def nsp_glu_bwd(dh, x, w_gate, w_up, g, u, dx, dw_gate, dw_up, ws, act=NSP_ACT_SILU, stream=None):
+    """Backward pass of nsp_glu_fwd from dh and the g, u it saved: dx (None: not wanted), dw_gate and dw_up (both None: not
+    wanted), overwritten. ws: a CUDA tensor of at least nsp_glu_bwd_ws_bytes(rows, d_model, d_ff) bytes."""
+    import torch
+
+    what = "nsp_glu_bwd"
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    _on_device(what, (("dh", dh), ("x", x), ("w_gate", w_gate), ("w_up", w_up), ("g", g), ("u", u), ("dx", dx), ("dw_gate", dw_gate),
+                      ("dw_up", dw_up), ("ws", ws)), here)
+    rows, d, f = _glu_sizes(what, x, w_gate)
+    _check_ws(what, ws)
+    rc = lib().nsp_glu_bwd(_matrix(what, "dh", dh, rows, f), _matrix(what, "x", x, rows, d), _matrix(what, "w_gate", w_gate, f, d),
+                           _matrix(what, "w_up", w_up, f, d), _matrix(what, "g", g, rows, f), _matrix(what, "u", u, rows, f),
+                           _matrix(what, "dx", dx, rows, d), _matrix(what, "dw_gate", dw_gate, f, d), _matrix(what, "dw_up", dw_up, f, d),
+                           rows, d, f, int(act), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream))
+    if rc != NSP_OK:
+        raise NspError(rc, what)
+
+
+def nsp_glu_status():
+    """The record of the nsp_glu calls on the current device, (code, tile, where, aux); code 0 = healthy. Synchronises."""
+    out = (ctypes.c_int32 * 4)()
+    rc = lib().nsp_glu_status(out)
+    if rc != NSP_OK:
+        raise NspError(rc, "nsp_glu_status")
+    return tuple(out)

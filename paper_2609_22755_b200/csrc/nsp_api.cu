@@ -17,6 +17,18 @@
 namespace nsp {
 static std::atomic<int64_t> g_launches{0};
 void count_launches(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
+
+TensorMapEncoder tensor_map_encoder() {
+  static TensorMapEncoder fn = nullptr;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<TensorMapEncoder>(p);
+  }
+  return fn;
+}
 }  // namespace nsp
 
 using namespace nsp;
@@ -92,26 +104,10 @@ struct nsp_plan {
 
 namespace {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
-
 // Tensor map of one run: a dense bf16 [tokens, heads, 128] tensor; tiles are {64 dims, 1 head, `rows` tokens}
 // with 128-byte swizzle, rows past the run read as zero.
 bool encode_run_map(CUtensorMap* out, const void* base, int64_t elem_off, int64_t tokens, int heads, int head_dim, int rows = kBM) {
-  EncodeTiledFn enc = get_encode_fn();
+  TensorMapEncoder enc = tensor_map_encoder();
   if (!enc) return false;
   if (tokens <= 0) {
     std::memset(out, 0, sizeof(*out));
@@ -132,7 +128,7 @@ bool encode_run_map(CUtensorMap* out, const void* base, int64_t elem_off, int64_
 // swizzle or row after row
 bool encode_run_map_f32(CUtensorMap* out, void* base, int64_t elem_off, int64_t tokens, int heads, int head_dim, int rows = 128,
                         bool swizzled = true) {
-  EncodeTiledFn enc = get_encode_fn();
+  TensorMapEncoder enc = tensor_map_encoder();
   if (!enc) return false;
   if (tokens <= 0) {
     std::memset(out, 0, sizeof(*out));

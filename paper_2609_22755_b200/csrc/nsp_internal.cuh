@@ -107,6 +107,11 @@ enum DeviceWhere : int32_t {
   kWhereCheckBwdDq = 42,
   kWhereCheckBwdDkv = 43,
   kWhereCheckBwdLse = 44,
+  kWhereGluSetup = 50,  // products of the feed-forward block: shared memory or TMEM not where they should be,
+  kWhereGluEmpty = 51,  // a stage whose products do not complete, operands that do not arrive, an accumulator that is not read,
+  kWhereGluFull = 52,   // one that is not completed
+  kWhereGluAccEmpty = 53,
+  kWhereGluAccFull = 54,
   kWhereSelfTest = 90,
 };
 
@@ -257,5 +262,11 @@ cudaError_t launch_bwd_postprocess(const SegInfo* d_seg, int n_seg, const int64_
                                    int head_dim, const float* dq_acc, void* dq, int dq_f32, float scale,
                                    cudaStream_t st);
 void count_launches(int n);
+
+// The driver's cuTensorMapEncodeTiled; null without a driver.
+typedef CUresult (*TensorMapEncoder)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                     const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                     CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+TensorMapEncoder tensor_map_encoder();
 
 }  // namespace nsp
