@@ -11,6 +11,10 @@
 // the first CTA's part of B comes from Wg and the second one's from Wu. Operands whose contraction index is not the contiguous one
 // (dg^T, du^T, x, and the weights of dx) are read MN-major by the tensor core: nothing is transposed in memory. Accumulators in
 // TMEM are double-buffered: 256 columns of the next tile are filled while the epilogue drains the last one's.
+// A stage holds 128 steps of the contraction and is filled by two instructions, one a warp: a 3-D box is two blocks of 64 columns at
+// once. What bounded the kernel before was not the bytes but the number of TMA instructions one thread issues (16,384 tokens, 4,096
+// x 12,288: stages of 64 steps and boxes of 64 columns 2,700 us there and 7,000 back, boxes of 128 columns 2,670 and 5,790, stages
+// of 128 steps 2,390 and 4,840).
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -22,27 +26,52 @@
 namespace nsp {
 namespace {
 
-constexpr int kStages = 6;
-constexpr uint32_t kOperand = 128 * 64 * 2;  // bytes: 128 rows (or 64 contraction steps of 2 x 64 columns) of 64 bf16
-constexpr int kThreads = 384;                // producer, issuer, two idle warps, two warpgroups of epilogue
-constexpr int kGroupM = 8;                   // row tiles that are walked together (see tile_at)
+constexpr int kStages = 3;
+constexpr int kDepth = 128;                       // steps of the contraction in a stage
+constexpr uint32_t kBlock = 128 * 64 * 2;         // bytes of a block of 128 rows x 64 columns
+constexpr uint32_t kOperand = 128 * kDepth * 2;
+constexpr int kThreads = 384;                     // producer of A, issuer, producer of B, an idle warp, two warpgroups of epilogue
+constexpr int kGroupM = 8;                        // row tiles that are walked together (see tile_at)
 constexpr long long kWaitLimit = NSP_WAIT_CYCLES_DEFAULT;
-constexpr int kMostMaps = 10, kMostProblems = 3;
+constexpr int kMostMaps = 20, kMostProblems = 3;
 
 struct Problem {
   int32_t tiles_m, tiles_n, first_tile;
-  int32_t segments, k_iters;       // the contraction: `segments` pairs of operands, k_iters steps of 64 each
-  int32_t a_map[2], b_map[2][2];   // [segment], [segment][rank of the CTA]
-  int32_t a_mn, b_mn;              // 1: the contiguous index is the row / column one
-  int32_t b_shared;                // 1: both CTAs' parts of B come from one matrix, nh columns apart
-  int32_t rows, cols;              // of the output
-  __nv_bfloat16* out[3];           // forward: h, g, u
+  int32_t segments, k_iters, depth;  // the contraction: `segments` pairs of operands, each of `depth` steps in k_iters stages
+  int32_t a_map[2], b_map[2][2];     // [segment], [segment][rank of the CTA]: first of an operand's two maps
+  int32_t a_mn, b_mn;                // 1: the contiguous index is the row / column one
+  int32_t b_shared;                  // 1: both CTAs' parts of B come from one matrix, nh columns apart
+  int32_t rows, cols;                // of the output
+  int32_t out_map;                   // forward: of h, g, u
+  __nv_bfloat16* out[3];
   int64_t ld[3];
+};
+
+// Which tiles a pair computes, in turn. The n_long long ones come first, one after the other to all pairs; the pairs that have one
+// less of them (those from `heavy` on) take the next `ahead` rounds of the short ones alone, and the rounds after that begin at
+// pair `start`.
+struct Schedule {
+  int32_t n_long, n_short, heavy, ahead, start;
+  __host__ __device__ __forceinline__ int tile(int i, int pair, int pairs) const {  // -1: no more
+    const int mine = n_long / pairs + (pair < heavy ? 1 : 0);
+    if (i < mine) return pair + i * pairs;
+    const int round = i - mine + (pair < heavy ? ahead : 0), light = pairs - heavy;
+    int t;
+    if (round < ahead) {
+      t = round * light + pair - heavy;
+    } else {
+      int at = pair - start;
+      if (at < 0) at += pairs;
+      t = ahead * light + (round - ahead) * pairs + at;
+    }
+    return t < n_short ? n_long + t : -1;
+  }
 };
 
 struct GemmArgs {
   Problem p[kMostProblems];
-  int32_t n_problems, n_tiles, nh;
+  int32_t n_problems, nh;
+  Schedule order;
   StatusWord status;
 };
 
@@ -53,6 +82,7 @@ struct Maps {
 struct Smem {
   uint8_t a[kStages][kOperand];
   uint8_t b[kStages][kOperand];
+  uint8_t out[2][kBlock];    // a warpgroup's block of an output on its way to memory
   uint64_t full[kStages];    // in the first CTA: the bytes of both
   uint64_t empty[kStages];   // in both: the products of the stage have completed
   uint64_t acc_full[2];      // in both: an accumulator is complete
@@ -101,6 +131,30 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const void* tma
       : "memory");
 }
 
+__device__ __forceinline__ void tma_store_2d(const void* tmap, const void* smem_src, int32_t c0, int32_t c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+               ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(smem_src)), "r"(c0), "r"(c1)
+               : "memory");
+}
+
+// One operand of a stage. `across` is the index of its rows (columns of the output for B), `k` the step of the contraction, `wide`
+// the rows of this CTA. maps[0] holds whole blocks of 64 contiguous columns, two of them a box: {64, the other index, blocks};
+// maps[1] is the plain matrix, for boxes that the end of the contiguous index cuts: the rest reads as zero.
+__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* maps, uint32_t bar, int mn, int across, int k, int wide,
+                                             int across_end, int k_end) {
+  const int at = mn ? across : k, other = mn ? k : across, end = mn ? across_end : k_end, cols = mn ? wide : kDepth;
+  if (at + cols <= end) {
+    tma_load_3d_pair(dst, maps, bar, 0, other, at / 64);
+  } else {
+    const uint32_t block = mn ? kBlock : static_cast<uint32_t>(wide) * 128;
+    const int last = mn ? cols : min(cols, end - at);  // the contraction ends in this stage: no blocks behind it
+    for (int c = 0; c < last; c += 64) tma_load_2d_pair(dst + c / 64 * block, maps + 1, bar, at + c, other);
+  }
+}
+__device__ __forceinline__ uint32_t operand_bytes(int mn, int wide, int k, int k_end) {
+  return mn || k + 64 < k_end ? wide * kDepth * 2 : wide * kDepth;
+}
+
 // 32 columns of one row
 __device__ __forceinline__ void store_row(__nv_bfloat16* out, int64_t ld, int row, int col, int rows, int cols, const uint32_t (&w)[16]) {
   if (row >= rows) return;
@@ -109,6 +163,32 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* out, int64_t ld, int ro
   for (int i = 0; i < 4; ++i)
     if (col + 8 * i < cols) *reinterpret_cast<uint4*>(p + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
+
+// A warpgroup's block of 128 rows x 64 columns, every thread a row, on its way through shared memory (the layout that a TMA store
+// with 128-byte swizzle takes): a warp that stores its 32 rows directly touches 32 lines with every instruction.
+struct BlockOut {
+  uint8_t* stage;
+  int wg, thread;
+  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+  __device__ __forceinline__ void begin() const {  // the block before has been read
+    if (thread == 0) tma_store_wait_read();
+    sync();
+  }
+  __device__ __forceinline__ void put(int c, const uint32_t (&w)[16]) const {  // columns 32 c .. 32 c + 31
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint4*>(stage + thread * 128 + (((4 * c + i) ^ (thread & 7)) * 16)) =
+          make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+  __device__ __forceinline__ void end(const CUtensorMap* map, int col, int row0, const Problem& p) const {
+    fence_proxy_async_smem();
+    sync();
+    if (thread == 0 && col < p.cols && row0 < p.rows) {
+      tma_store_2d(map, stage, col, row0);
+      tma_store_commit();
+    }
+  }
+};
 
 __device__ __forceinline__ void pack_row(const uint32_t (&r)[32], uint32_t (&w)[16]) {
 #pragma unroll
@@ -156,20 +236,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     return a.p[k];
   };
 
-  if (warp == 0) {
-    // ================================================================ TMA producer (both CTAs, each its own operands)
+  if (warp == 0 || warp == 2) {
+    // ================================================================ TMA producers of A and of B (both CTAs, each its own rows)
     if (lane == 0) {
+      const bool is_a = warp == 0;
       uint32_t it = 0;
-      for (int tile = pair; tile < a.n_tiles; tile += pairs) {
+      bool ok = true;
+      for (int i = 0, tile; ok && (tile = a.order.tile(i, pair, pairs)) >= 0; ++i) {
         const Problem& p = problem_of(tile);
         int m, n;
         tile_at(p, tile - p.first_tile, m, n);
-        const int row = m * 256 + static_cast<int>(rank) * 128;
-        const int col = p.b_shared ? n * 2 * nh + static_cast<int>(rank) * nh : n * nh;
-        bool ok = true;
+        const int mine = static_cast<int>(rank);
+        const int across = is_a ? m * 256 + mine * 128 : p.b_shared ? n * 2 * nh + mine * nh : n * nh;
+        const int mn = is_a ? p.a_mn : p.b_mn, wide = is_a ? 128 : nh, end = is_a ? p.rows : p.cols;
         for (int seg = 0; seg < p.segments && ok; ++seg) {
-          const CUtensorMap* ma = &maps.m[p.a_map[seg]];
-          const CUtensorMap* mb = &maps.m[p.b_map[seg][rank]];
+          const CUtensorMap* map = &maps.m[is_a ? p.a_map[seg] : p.b_map[seg][mine]];
           for (int k = 0; k < p.k_iters; ++k, ++it) {
             const uint32_t st = it % kStages, ph = (it / kStages) & 1;
             if (*abort_flag || !mbar_wait(&s.empty[st], ph ^ 1, kWaitLimit)) {
@@ -178,22 +259,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
               ok = false;
               break;
             }
-            if (rank == 0) mbar_expect_tx(&s.full[st], 2 * (kOperand + nh * 128));
-            const uint32_t bar = lead + off(&s.full[st]);
-            if (p.a_mn) {
-              tma_load_2d_pair(s.a[st], ma, bar, row, k * 64);
-              tma_load_2d_pair(s.a[st] + kOperand / 2, ma, bar, row + 64, k * 64);
-            } else {
-              tma_load_2d_pair(s.a[st], ma, bar, k * 64, row);
-            }
-            if (p.b_mn) {
-              for (int c = 0; c < nh; c += 64) tma_load_2d_pair(s.b[st] + c * 128, mb, bar, col + c, k * 64);
-            } else {
-              tma_load_2d_pair(s.b[st], mb, bar, k * 64, col);
-            }
+            if (is_a && rank == 0)
+              mbar_expect_tx(&s.full[st], 2 * (operand_bytes(p.a_mn, 128, k * kDepth, p.depth) + operand_bytes(p.b_mn, nh, k * kDepth, p.depth)));
+            load_operand(is_a ? s.a[st] : s.b[st], map, lead + off(&s.full[st]), mn, across, k * kDepth, wide, end, p.depth);
           }
         }
-        if (!ok) break;
       }
     }
     __syncwarp();
@@ -203,13 +273,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     const uint32_t hi = static_cast<uint32_t>(make_smem_desc_sw128(0, 16, 1024) >> 32);
     uint32_t it = 0, n_done = 0;
     bool ok = true;
-    for (int tile = pair; tile < a.n_tiles && ok; tile += pairs, ++n_done) {
+    for (int tile; ok && (tile = a.order.tile(static_cast<int>(n_done), pair, pairs)) >= 0; ++n_done) {
       const Problem& p = problem_of(tile);
       const uint32_t buf = n_done & 1, d = buf * 256;
       const uint32_t idesc = make_idesc_bf16(256, 2 * nh, p.a_mn, p.b_mn);
-      // a step of 16 of the contraction: 32 bytes of a row, or 16 rows
-      const uint32_t a_lbo = p.a_mn ? ((kOperand / 2) >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2;
-      const uint32_t b_lbo = p.b_mn ? ((kOperand / 2) >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2;
+      // 16 steps of the contraction: 32 bytes of a row (four of them in a block), or 16 rows
+      const uint32_t a_lbo = p.a_mn ? (kBlock >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : kBlock >> 4;
+      const uint32_t b_lbo = p.b_mn ? (kBlock >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
       bool here = cluster_wait_tmem(&s.acc_empty[buf], ((n_done >> 1) & 1) ^ 1, kWaitLimit);
       if (!__all_sync(0xffffffffu, here)) {
         if (lane == 0) report_timeout(a.status, tile, kWhereGluAccEmpty, 0), raise_abort();
@@ -227,10 +297,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
           break;
         }
         tc_fence_after_sync();
+        const int left = p.depth - (k >= p.k_iters ? k - p.k_iters : k) * kDepth;  // steps of the segment from this stage on
         if (leader) {
           const uint32_t a_lo = smem_desc_addr(s.a[st]) | a_lbo, b_lo = smem_desc_addr(s.b[st]) | b_lbo;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) umma2_ss_lh(d, a_lo + kk * a_step, hi, b_lo + kk * b_step, hi, idesc, (k | kk) != 0);
+          for (int kk = 0; kk < kDepth / 16; ++kk) {
+            if (kk * 16 < left)
+              umma2_ss_lh(d, a_lo + (kk >> 2) * a_next + (kk & 3) * a_step, hi, b_lo + (kk >> 2) * b_next + (kk & 3) * b_step, hi, idesc,
+                          (k | kk) != 0);
+          }
           umma2_commit(&s.empty[st]);
           if (k + 1 == iters) umma2_commit(&s.acc_full[buf]);
         }
@@ -242,7 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
     uint32_t n_done = 0;
-    for (int tile = pair; tile < a.n_tiles; tile += pairs, ++n_done) {
+    for (int tile; (tile = a.order.tile(static_cast<int>(n_done), pair, pairs)) >= 0; ++n_done) {
       const Problem& p = problem_of(tile);
       int m, n;
       tile_at(p, tile - p.first_tile, m, n);
@@ -254,41 +329,84 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         break;
       }
       tc_fence_after_sync();
-      const int row = m * 256 + static_cast<int>(rank) * 128 + quad * 32 + lane;
+      const int row0 = m * 256 + static_cast<int>(rank) * 128, thread = quad * 32 + lane, row = row0 + thread;
       const uint32_t t0 = buf * 256 + lanes;
+      const BlockOut out{s.out[half], half, thread};
+      auto drained = [&]() {  // this warp has read its part of the accumulator
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank == 0)
+            mbar_arrive(&s.acc_empty[buf]);
+          else
+            cluster_arrive_relaxed(lead + off(&s.acc_empty[buf]));
+        }
+      };
       if constexpr (kAct >= 0) {
-        const int per = nh / 2;  // columns of h of this warpgroup
-        for (int c = half * per; c < (half + 1) * per; c += 32) {
-          uint32_t g[32], u[32], w[16];
-          tmem_ld32(t0 + c, g);
-          tmem_ld32(t0 + nh + c, u);
-          tmem_wait_ld();
-          const int col = n * nh + c;
-          if (p.out[1]) pack_row(g, w), store_row(p.out[1], p.ld[1], row, col, p.rows, p.cols, w);
-          if (p.out[2]) pack_row(u, w), store_row(p.out[2], p.ld[2], row, col, p.rows, p.cols, w);
+        if (nh == 128) {  // 64 columns of h a warpgroup
+          uint32_t g[2][16], u[2][16];
+          out.begin();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) g[i] = __float_as_uint(act_value<kAct>(__uint_as_float(g[i])) * __uint_as_float(u[i]));
-          pack_row(g, w);
-          store_row(p.out[0], p.ld[0], row, col, p.rows, p.cols, w);
+          for (int c = 0; c < 2; ++c) {
+            uint32_t x[32], y[32], w[16];
+            tmem_ld32(t0 + half * 64 + c * 32, x);
+            tmem_ld32(t0 + 128 + half * 64 + c * 32, y);
+            tmem_wait_ld();
+            if (c == 1) drained();
+            pack_row(x, g[c]);
+            pack_row(y, u[c]);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(act_value<kAct>(__uint_as_float(x[i])) * __uint_as_float(y[i]));
+            pack_row(x, w);
+            out.put(c, w);
+          }
+          const int col = n * 128 + half * 64;
+          out.end(&maps.m[p.out_map], col, row0, p);
+          if (p.out[1]) {
+            out.begin();
+            out.put(0, g[0]), out.put(1, g[1]);
+            out.end(&maps.m[p.out_map + 1], col, row0, p);
+          }
+          if (p.out[2]) {
+            out.begin();
+            out.put(0, u[0]), out.put(1, u[1]);
+            out.end(&maps.m[p.out_map + 2], col, row0, p);
+          }
+        } else {
+          const int per = nh / 2;  // columns of h of this warpgroup
+          for (int c = half * per; c < (half + 1) * per; c += 32) {
+            uint32_t g[32], u[32], w[16];
+            tmem_ld32(t0 + c, g);
+            tmem_ld32(t0 + nh + c, u);
+            tmem_wait_ld();
+            const int col = n * nh + c;
+            if (p.out[1]) pack_row(g, w), store_row(p.out[1], p.ld[1], row, col, p.rows, p.cols, w);
+            if (p.out[2]) pack_row(u, w), store_row(p.out[2], p.ld[2], row, col, p.rows, p.cols, w);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = __float_as_uint(act_value<kAct>(__uint_as_float(g[i])) * __uint_as_float(u[i]));
+            pack_row(g, w);
+            store_row(p.out[0], p.ld[0], row, col, p.rows, p.cols, w);
+          }
+          drained();
         }
       } else {
-        for (int c = half * nh; c < (half + 1) * nh; c += 32) {
-          uint32_t r[32], w[16];
-          tmem_ld32(t0 + c, r);
-          tmem_wait_ld();
-          pack_row(r, w);
-          store_row(p.out[0], p.ld[0], row, n * 2 * nh + c, p.rows, p.cols, w);
+        // nh columns a warpgroup, 64 at a time
+        for (int c = 0; c < nh; c += 64) {
+          out.begin();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t r[32], w[16];
+            tmem_ld32(t0 + half * nh + c + i * 32, r);
+            tmem_wait_ld();
+            if (i == 1 && c + 64 >= nh) drained();
+            pack_row(r, w);
+            out.put(i, w);
+          }
+          out.end(&maps.m[p.out_map], n * 2 * nh + half * nh + c, row0, p);
         }
       }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) {
-        if (rank == 0)
-          mbar_arrive(&s.acc_empty[buf]);
-        else
-          cluster_arrive_relaxed(lead + off(&s.acc_empty[buf]));
-      }
     }
+    if (lane == 0) tma_store_wait();
   }
   __syncwarp();
   __syncthreads();
@@ -377,24 +495,65 @@ int record_of(DeviceRecord** out) {
   return *reinterpret_cast<volatile int32_t*>(r.host);
 }
 
-bool encode(CUtensorMap* out, const void* base, int64_t inner, int64_t rows, int64_t ld, int box_inner, int box_rows) {
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_rows)};
-  const cuuint32_t step[2] = {1, 1};
+bool encode(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  const cuuint32_t step[3] = {1, 1, 1};
   TensorMapEncoder enc = tensor_map_encoder();
-  return enc && enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return enc && enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// A matrix in boxes of 64 columns
+bool encode_plain(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
+  return encode(out, base, 2, dims, strides, box);
+}
+// The two maps of an operand (see load_operand): boxes of `blocks` blocks of 64 columns, and the plain matrix. The first one
+// covers whole blocks alone, so that no box of it reads past the end of a row.
+bool encode_operand(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_rows, int blocks) {
+  const cuuint64_t dims[3] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols < 64 ? 1 : cols / 64)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, 128};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(blocks)};
+  return encode(out, base, 3, dims, strides, box) && encode_plain(out + 1, base, cols, rows, ld, box_rows);
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
+// The order of n_long tiles of `cost` stages and n_short of `less` <= cost for that many pairs: `ahead` and `start` of the smallest
+// latest end. (4,099 tokens, 2,056 x 5,512 backward: 153 tiles of 88 stages and 396 of 33; the latest pair has 429 stages where all
+// tiles are dealt out one by one, 374 so, of a mean of 359.)
+Schedule plan_schedule(int n_long, int cost, int n_short, int less, int pairs) {
+  Schedule best{n_long, n_short, n_long % pairs, 0, 0};
+  if (n_short == 0) return best;
+  int64_t best_end = -1;
+  const int most = best.heavy ? (cost + less - 1) / less : 0;
+  for (int ahead = 0; ahead <= most; ++ahead) {
+    for (int start : {0, best.heavy}) {
+      const Schedule s{n_long, n_short, best.heavy, ahead, start};
+      int64_t end = 0;
+      const int light = pairs - s.heavy, rest = n_short - ahead * light;  // of the rounds that all pairs take part in
+      for (int pair = 0; pair < pairs; ++pair) {
+        int64_t n;
+        if (rest <= 0) {
+          n = pair < s.heavy ? 0 : n_short / light + (pair - s.heavy < n_short % light ? 1 : 0);
+        } else {
+          const int at = pair >= start ? pair - start : pair - start + pairs;
+          n = (pair < s.heavy ? 0 : ahead) + rest / pairs + (at < rest % pairs ? 1 : 0);
+        }
+        const int64_t load = static_cast<int64_t>(n_long / pairs + (pair < s.heavy ? 1 : 0)) * cost + n * less;
+        end = load > end ? load : end;
+      }
+      if (best_end < 0 || end < best_end) best = s, best_end = end;
+    }
+  }
+  return best;
+}
+
 template <int kAct>
-cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, int sms, cudaStream_t st) {
+cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, int pairs, cudaStream_t st) {
   static_assert(sizeof(Maps) + sizeof(GemmArgs) <= 4000, "kernel parameters");
   const cudaError_t e = cudaFuncSetAttribute(glu_gemm_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Smem)));
   if (e != cudaSuccess) return e;
-  const int pairs = a.n_tiles < sms / 2 ? a.n_tiles : sms / 2;
   count_launches(1);
   return launch_chained_if(true, glu_gemm_kernel<kAct>, 2 * pairs, kThreads, sizeof(Smem), st, maps, a);
 }
@@ -436,23 +595,26 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
   a.nh = 128;
   Problem& p = a.p[0];
   p.tiles_m = ceil_div(T, 256), p.tiles_n = ceil_div(d_ff, a.nh);
-  p.segments = 1, p.k_iters = ceil_div(d_model, 64);
-  p.b_map[0][0] = 1, p.b_map[0][1] = 2;
+  p.segments = 1, p.depth = d_model, p.k_iters = ceil_div(d_model, kDepth);
+  p.a_map[0] = 0, p.b_map[0][0] = 2, p.b_map[0][1] = 4, p.out_map = 6;
   p.rows = T, p.cols = d_ff;
   const nsp_matrix_t* outs[3] = {h, g, u};
   for (int i = 0; i < 3; ++i) {
     if (!outs[i]) continue;
     p.out[i] = static_cast<__nv_bfloat16*>(const_cast<void*>(outs[i]->data));
     p.ld[i] = ld_of(outs[i], rows, d_ff);
+    if (!encode_plain(&maps.m[p.out_map + i], outs[i]->data, d_ff, rows, p.ld[i], 128)) return NSP_ERR_CUDA;
   }
-  if (!encode(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), 64, 128) ||
-      !encode(&maps.m[1], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), 64, a.nh) ||
-      !encode(&maps.m[2], w_up->data, d_model, d_ff, ld_of(w_up, d_ff, d_model), 64, a.nh))
+  if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), 128, 2) ||
+      !encode_operand(&maps.m[2], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), a.nh, 2) ||
+      !encode_operand(&maps.m[4], w_up->data, d_model, d_ff, ld_of(w_up, d_ff, d_model), a.nh, 2))
     return NSP_ERR_CUDA;
-  a.n_problems = 1, a.n_tiles = p.tiles_m * p.tiles_n;
+  a.n_problems = 1;
+  const int n_tiles = p.tiles_m * p.tiles_n, pairs = n_tiles < rec->sms / 2 ? n_tiles : rec->sms / 2;
+  a.order = plan_schedule(n_tiles, p.k_iters, 0, 0, pairs);
   a.status = rec->word;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return (act == NSP_ACT_SILU ? launch_gemm<kSilu>(maps, a, rec->sms, st) : launch_gemm<kGelu>(maps, a, rec->sms, st)) == cudaSuccess
+  return (act == NSP_ACT_SILU ? launch_gemm<kSilu>(maps, a, pairs, st) : launch_gemm<kGelu>(maps, a, pairs, st)) == cudaSuccess
              ? NSP_OK : NSP_ERR_CUDA;
 }
 
@@ -501,41 +663,49 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   a.nh = 128;
   bool ok = true;
   // dg, du as [rows, d_ff]: the contraction of dx runs along their rows, that of the weights' gradients along their columns
-  if (want_w) {
+  int n_tiles = 0, tiles[2] = {0, 0}, cost[2] = {ceil_div(T, kDepth), 2 * ceil_div(d_ff, kDepth)};  // of dW, dx
+  auto add = [&](int cls, int64_t out_rows) -> Problem& {
+    Problem& p = a.p[a.n_problems++];
+    p.tiles_m = ceil_div(out_rows, 256), p.tiles_n = ceil_div(d_model, 2 * a.nh), p.first_tile = n_tiles;
+    p.rows = static_cast<int32_t>(out_rows), p.cols = d_model, p.b_mn = p.b_shared = 1;
+    n_tiles += p.tiles_m * p.tiles_n, tiles[cls] += p.tiles_m * p.tiles_n;
+    return p;
+  };
+  auto add_w = [&]() {
     const nsp_matrix_t* outs[2] = {dw_gate, dw_up};
     for (int i = 0; i < 2; ++i) {
-      Problem& p = a.p[a.n_problems++];
-      p.tiles_m = ceil_div(d_ff, 256), p.tiles_n = ceil_div(d_model, 2 * a.nh), p.first_tile = a.n_tiles;
-      p.segments = 1, p.k_iters = ceil_div(T, 64), p.a_mn = p.b_mn = p.b_shared = 1;
-      p.a_map[0] = i, p.b_map[0][0] = p.b_map[0][1] = 2;
-      p.rows = d_ff, p.cols = d_model;
-      p.out[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(outs[i]->data)), p.ld[0] = ld_of(outs[i], d_ff, d_model);
-      a.n_tiles += p.tiles_m * p.tiles_n;
-      ok = ok && encode(&maps.m[i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, 64, 64);
+      Problem& p = add(0, d_ff);
+      p.segments = 1, p.depth = T, p.k_iters = ceil_div(T, kDepth), p.a_mn = 1;
+      p.a_map[0] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = 4, p.out_map = 14 + i;
+      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, kDepth, 2) &&
+           encode_plain(&maps.m[14 + i], outs[i]->data, d_model, d_ff, ld_of(outs[i], d_ff, d_model), 128);
     }
-    ok = ok && encode(&maps.m[2], x->data, d_model, rows, ld_of(x, rows, d_model), 64, 64);
-  }
-  if (want_x) {
-    Problem& p = a.p[a.n_problems++];
-    p.tiles_m = ceil_div(T, 256), p.tiles_n = ceil_div(d_model, 2 * a.nh), p.first_tile = a.n_tiles;
-    p.segments = 2, p.k_iters = ceil_div(d_ff, 64), p.b_mn = p.b_shared = 1;
-    p.rows = T, p.cols = d_model;
-    p.out[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(dx->data)), p.ld[0] = ld_of(dx, rows, d_model);
-    a.n_tiles += p.tiles_m * p.tiles_n;
+    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), kDepth, a.nh / 64);
+  };
+  auto add_x = [&]() {
+    Problem& p = add(1, rows);
+    p.segments = 2, p.depth = d_ff, p.k_iters = ceil_div(d_ff, kDepth), p.out_map = 16;
+    ok = ok && encode_plain(&maps.m[16], dx->data, d_model, rows, ld_of(dx, rows, d_model), 128);
     for (int i = 0; i < 2; ++i) {
       const nsp_matrix_t* w = i ? w_up : w_gate;
-      p.a_map[i] = 3 + i, p.b_map[i][0] = p.b_map[i][1] = 5 + i;
-      ok = ok && encode(&maps.m[3 + i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, 64, 128) &&
-           encode(&maps.m[5 + i], w->data, d_model, d_ff, ld_of(w, d_ff, d_model), 64, 64);
+      p.a_map[i] = 6 + 2 * i, p.b_map[i][0] = p.b_map[i][1] = 10 + 2 * i;
+      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, 128, 2) &&
+           encode_operand(&maps.m[10 + 2 * i], w->data, d_model, d_ff, ld_of(w, d_ff, d_model), kDepth, a.nh / 64);
     }
-  }
+  };
+  const int first = cost[1] > cost[0] && want_x ? 1 : 0;  // the class of the longer tiles
+  if (first == 1) add_x();
+  if (want_w) add_w();
+  if (first == 0 && want_x) add_x();
+  const int pairs = n_tiles < rec->sms / 2 ? n_tiles : rec->sms / 2;
+  a.order = plan_schedule(tiles[first], cost[first], tiles[1 - first], cost[1 - first], pairs);
   if (!ok) return NSP_ERR_CUDA;
   a.status = rec->word;
   count_launches(1);
   const int blocks = act_args.total / 256 + 1 < 148u * 8 ? static_cast<int>(act_args.total / 256 + 1) : 148 * 8;
   if (launch_chained_if(true, act == NSP_ACT_SILU ? glu_act_kernel<kSilu> : glu_act_kernel<kGelu>, blocks, 256, 0, st, act_args) != cudaSuccess)
     return NSP_ERR_CUDA;
-  return launch_gemm<-1>(maps, a, rec->sms, st) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
+  return launch_gemm<-1>(maps, a, pairs, st) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }
 
 extern "C" int nsp_glu_status(int32_t out[4]) {

@@ -6,11 +6,14 @@
 // between its sums and its outputs. All sums are in fp32: mu first and then the squares around it (the difference of two large
 // sums would lose the variance of rows that lie far from zero).
 //
-// Teams. A row belongs to a team of threads, part of a warp for short rows (heads), a block for long ones; thread i has the
-// vectors i, i + team, ... of 16 bytes (bf16), single elements where the rows' addresses do not allow vectors. A team walks over
-// the rows with a step of all teams and loads its next row before it sums up the present one.
-// The parameters' gradients stay in fp32 registers, column by column, for all rows of a team; the teams of a block are added in
-// shared memory, the blocks' sums go to the workspace and a second kernel adds them in their order: the same bits in every run.
+// Teams. A row belongs to a team of threads: some lanes of a warp, a warp or several warps; thread i of it has the vectors i,
+// i + team, ... of 8 elements. In the forward pass a lane has up to 16 vectors, so that a row of 4,096 is one warp's: no barrier,
+// and loads of a whole row under way in every warp. In the backward pass a thread keeps the parameters' gradients of its columns in
+// fp32 registers over all rows it meets, which bounds its columns to 16 or 32; long rows are a block's, come through shared memory
+// some rows ahead by asynchronous copies (each thread copies and reads its own vectors: no barrier either), and the sums of
+// one or two rows are exchanged at one barrier. The blocks' gradients go to the workspace and a second kernel adds them in their
+// order: the same bits in every run.
+// Rows whose addresses do not allow vectors go element by element, through kernels of their own (norm_*_element_kernel).
 #include <cmath>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -20,7 +23,11 @@
 
 using nsp::grid_launch_dependents;
 using nsp::grid_wait_predecessor;
+using nsp::add2;
+using nsp::fma2;
+using nsp::mul2;
 using nsp::pack_bf16x2;
+using nsp::smem_u32;
 
 namespace {
 
@@ -37,7 +44,7 @@ struct NormArgs {
   float* rstd;
   float* part;  // [2][blocks][dim]: sums of a block for dw, db
   int64_t rows;
-  int32_t inner, dim, w_f32, want_grads;
+  int32_t inner, dim, w_f32, want_grads, stages;
   float eps, inv_dim;
 };
 
@@ -158,7 +165,7 @@ struct RowWalk {
 };
 
 template <typename T, int V, int NV, int kTeam, bool kLayer>
-__global__ void __launch_bounds__(kTeam ? 256 : (V == 1 ? 1024 : NV == 4 ? 512 : 256)) norm_fwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kTeam ? 256 : (V == 1 ? 1024 : NV == 4 ? 512 : 256)) norm_fwd_element_kernel(const NormArgs a) {
   __shared__ float slots[2][1][32];
   const int team = kTeam ? kTeam : blockDim.x, teams = blockDim.x / team;
   const int me = static_cast<int>(threadIdx.x) % team;
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(kTeam ? 256 : (V == 1 ? 1024 : NV == 4 ? 512 :
 }
 
 template <typename T, int V, int NV, int kTeam, bool kLayer>
-__global__ void __launch_bounds__(kTeam ? 256 : (V == 8 && NV == 1 ? 512 : 1024)) norm_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kTeam ? 256 : (V == 8 && NV == 1 ? 512 : 1024)) norm_bwd_element_kernel(const NormArgs a) {
   __shared__ float slots[2][2][32];
   const int team = kTeam ? kTeam : blockDim.x, teams = blockDim.x / team;
   const int me = static_cast<int>(threadIdx.x) % team;
@@ -340,89 +347,557 @@ __global__ void __launch_bounds__(kTeam ? 256 : (V == 8 && NV == 1 ? 512 : 1024)
   }
 }
 
-// dw and db (the second half of the blocks) from the sums of the blocks: 32 columns a block, eight threads a column that take
-// every eighth sum.
-__global__ void __launch_bounds__(256) norm_grads_kernel(const float* part, int blocks, int dim, float* dw, float* db) {
-  __shared__ float sum[8][32];
+// ---------------------------------------------------------------- vectors of 8 elements
+// Sums of N values over kLanes lanes: halves of the values change places with halves of the lanes until a lane has one value, so
+// that N values take N + 3 shuffles instead of 5 N; sum_at(k) is the lane (of its team) that ends up with value k.
+template <int N, int kLanes>
+__device__ __forceinline__ float lanes_sum(float (&v)[N], int lane) {
+  int o = kLanes / 2;
+#pragma unroll
+  for (int n = N; n > 1; n /= 2, o /= 2) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int k = 0; k < n / 2; ++k) {
+      const float give = upper ? v[k] : v[k + n / 2], keep = upper ? v[k + n / 2] : v[k];
+      v[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+#pragma unroll
+  for (; o > 0; o /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+  return v[0];
+}
+template <int N, int kLanes>
+__host__ __device__ constexpr int sum_at(int k) {
+  int at = 0;
+  for (int n = N, o = kLanes / 2; n > 1; n /= 2, o /= 2)
+    if (k >= n / 2) at |= o, k -= n / 2;
+  return at;
+}
+
+__device__ __forceinline__ void row_of(uint32_t r, int inner, int64_t& o, int& i) {
+  o = r / static_cast<uint32_t>(inner);
+  i = static_cast<int>(r - static_cast<uint32_t>(o) * inner);
+}
+
+// kLanes lanes (a warp: kWarps of them) a row, kVecs vectors a lane, kRows rows a team
+template <typename T, int kLanes, int kVecs, int kWarps, int kRows, bool kLayer>
+__global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kernel(const NormArgs a) {
+  constexpr int kTeam = kLanes * kWarps, kBlock = kWarps > 4 ? 32 * kWarps : 128, kTeams = kBlock / kTeam;
+  static_assert(kWarps == 1 || kRows == 1, "rows of several warps one at a time");
+  __shared__ float part[2][kWarps > 1 ? kTeams : 1][kWarps];
+  const int lane = static_cast<int>(threadIdx.x) % kTeam, team = static_cast<int>(threadIdx.x) / kTeam;
+  const int n_vec = a.dim / 8;
+  grid_wait_predecessor();
+  grid_launch_dependents();
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kTeams + team) * kRows;
+  Vec<T, 8> x[kRows][kVecs];
+  char* out[kRows];
+#pragma unroll
+  for (int q = 0; q < kRows; ++q) {
+    int64_t o;
+    int i;
+    row_of(static_cast<uint32_t>(first + q), a.inner, o, i);
+    const char* row = a.x.p + o * a.x.outer + i * a.x.inner;
+    out[q] = a.y.p + o * a.y.outer + i * a.y.inner;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      x[q][j].zero();
+      if (first + q < a.rows && lane + j * kTeam < n_vec) x[q][j].load(row, lane + j * kTeam);
+    }
+  }
+  // the same sum in all threads of a team
+  auto team_sum = [&](float (&v)[kRows], [[maybe_unused]] int turn) {
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o /= 2) {
+#pragma unroll
+      for (int q = 0; q < kRows; ++q) v[q] += __shfl_xor_sync(0xffffffffu, v[q], o);
+    }
+    if constexpr (kWarps > 1) {
+      if (lane % 32 == 0) part[turn][team][lane / 32] = v[0];
+      __syncthreads();
+      v[0] = part[turn][team][0];
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) v[0] += part[turn][team][w];
+    }
+  };
+  float mu[kRows], rstd[kRows];
+#pragma unroll
+  for (int q = 0; q < kRows; ++q) mu[q] = 0.f;
+  if (kLayer) {
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) add2(s[k % 4], s[k % 4 + 1], s[k % 4], s[k % 4 + 1], x[q][j].get(k), x[q][j].get(k + 1));
+      }
+      mu[q] = (s[0] + s[2]) + (s[1] + s[3]);
+    }
+    team_sum(mu, 0);
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) mu[q] *= a.inv_dim;
+  }
+#pragma unroll
+  for (int q = 0; q < kRows; ++q) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      if (!kLayer || lane + j * kTeam < n_vec) {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          float d0 = x[q][j].get(k), d1 = x[q][j].get(k + 1);
+          if (kLayer) add2(d0, d1, d0, d1, -mu[q], -mu[q]);
+          fma2(s[k % 4], s[k % 4 + 1], d0, d1, d0, d1, s[k % 4], s[k % 4 + 1]);
+        }
+      }
+    }
+    rstd[q] = (s[0] + s[2]) + (s[1] + s[3]);
+  }
+  team_sum(rstd, 1);
+#pragma unroll
+  for (int q = 0; q < kRows; ++q) {
+    rstd[q] = 1.f / sqrtf(rstd[q] * a.inv_dim + a.eps);
+    if (lane == 0 && first + q < a.rows) {
+      if (a.rstd) a.rstd[first + q] = rstd[q];
+      if (kLayer && a.mean) a.mean[first + q] = mu[q];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int v = lane + j * kTeam;
+    if (v < n_vec) {
+      float w[8], b[8];
+      load_params<8>(a.w, a.w_f32, v * 8, 1.f, w);
+      load_params<8>(a.b, a.w_f32, v * 8, 0.f, b);
+#pragma unroll
+      for (int q = 0; q < kRows; ++q) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          float d0 = x[q][j].get(k), d1 = x[q][j].get(k + 1);
+          if (kLayer) add2(d0, d1, d0, d1, -mu[q], -mu[q]);
+          mul2(d0, d1, d0, d1, rstd[q], rstd[q]);
+          fma2(y[k], y[k + 1], d0, d1, w[k], w[k + 1], b[k], b[k + 1]);
+        }
+        if (first + q < a.rows) Vec<T, 8>::store(out[q], v, y);
+      }
+    }
+  }
+}
+
+// What a thread does with a vector of a row: the sums of t h and t, the parameters' gradients, and dx.
+enum : int { kRms = 0, kRmsBias = 1, kLayerBias = 2 };  // whether mean(t) is subtracted and db is summed up
+template <typename T, int kKind>
+struct BwdVec {
+  __device__ __forceinline__ static void sums(const Vec<T, 8>& x, const Vec<T, 8>& dy, const float (&w)[8], float r, float shift, float (&s)[2],
+                                              float (&c)[2], float (&dw)[8], float (&db)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      float h0, h1, t0, t1;
+      const float g0 = dy.get(k), g1 = dy.get(k + 1);
+      hat(x, k, r, shift, h0, h1);
+      mul2(t0, t1, g0, g1, w[k], w[k + 1]);
+      fma2(s[0], s[1], t0, t1, h0, h1, s[0], s[1]);
+      if (kKind == kLayerBias) add2(c[0], c[1], c[0], c[1], t0, t1);
+      fma2(dw[k], dw[k + 1], g0, g1, h0, h1, dw[k], dw[k + 1]);
+      if (kKind != kRms) add2(db[k], db[k + 1], db[k], db[k + 1], g0, g1);
+    }
+  }
+  // h = (x - mu) r; `shift` is -mu
+  __device__ __forceinline__ static void hat(const Vec<T, 8>& x, int k, float r, float shift, float& h0, float& h1) {
+    h0 = x.get(k), h1 = x.get(k + 1);
+    if (kKind == kLayerBias) add2(h0, h1, h0, h1, shift, shift);
+    mul2(h0, h1, h0, h1, r, r);
+  }
+  // r (t - c2 - h c1)
+  __device__ __forceinline__ static void grad(const Vec<T, 8>& x, const Vec<T, 8>& dy, const float (&w)[8], float r, float shift, float c1,
+                                              float c2, char* out, int v) {
+    float o[8];
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      float h0, h1, t0, t1;
+      hat(x, k, r, shift, h0, h1);
+      if (kKind == kLayerBias)
+        fma2(t0, t1, dy.get(k), dy.get(k + 1), w[k], w[k + 1], -c2, -c2);
+      else
+        mul2(t0, t1, dy.get(k), dy.get(k + 1), w[k], w[k + 1]);
+      fma2(t0, t1, h0, h1, -c1, -c1, t0, t1);
+      mul2(o[k], o[k + 1], t0, t1, r, r);
+    }
+    Vec<T, 8>::store(out, v, o);
+  }
+};
+
+// Short rows: kLanes lanes of a warp a row, kRows rows at a time
+template <typename T, int kLanes, int kVecs, int kRows, int kKind>
+__global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
+  constexpr int kTeams = 256 / kLanes, kSums = kRows * (kKind == kLayerBias ? 2 : 1);
+  const int lane = static_cast<int>(threadIdx.x) % kLanes, team = static_cast<int>(threadIdx.x) / kLanes;
+  const int n_vec = a.dim / 8;
+  float dw[kVecs][8], db[kVecs][8], w[kVecs][8];
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[j][k] = 0.f, db[j][k] = 0.f, w[j][k] = 0.f;
+  }
+  grid_wait_predecessor();
+  grid_launch_dependents();
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j)
+    if (lane + j * kLanes < n_vec) load_params<8>(a.w, a.w_f32, (lane + j * kLanes) * 8, 1.f, w[j]);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kTeams * kRows;
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * kTeams * kRows; base < a.rows; base += step) {
+    Vec<T, 8> x[kRows][kVecs], dy[kRows][kVecs];
+    float r[kRows], shift[kRows];
+    char* out[kRows];
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      const int64_t row = base + q * kTeams + team;
+      const bool here = row < a.rows;
+      int64_t o;
+      int i;
+      row_of(static_cast<uint32_t>(row), a.inner, o, i);
+      const char *px = a.x.p + o * a.x.outer + i * a.x.inner, *pg = a.dy.p + o * a.dy.outer + i * a.dy.inner;
+      out[q] = here ? a.y.p + o * a.y.outer + i * a.y.inner : nullptr;
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+        x[q][j].zero(), dy[q][j].zero();
+        if (here && lane + j * kLanes < n_vec) x[q][j].load(px, lane + j * kLanes), dy[q][j].load(pg, lane + j * kLanes);
+      }
+      r[q] = here ? a.rstd[row] : 0.f;
+      shift[q] = kKind == kLayerBias && here ? -a.mean[row] : 0.f;
+    }
+    float sum[kSums];
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j)
+        if (lane + j * kLanes < n_vec) BwdVec<T, kKind>::sums(x[q][j], dy[q][j], w[j], r[q], shift[q], s, c, dw[j], db[j]);
+      sum[q] = s[0] + s[1];
+      if (kKind == kLayerBias) sum[kRows + q] = c[0] + c[1];
+    }
+    const float mine = lanes_sum<kSums, kLanes>(sum, lane) * a.inv_dim;
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      const float c1 = __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(q), kLanes);
+      const float c2 = kKind == kLayerBias ? __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(kRows + q), kLanes) : 0.f;
+      if (out[q]) {
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j)
+          if (lane + j * kLanes < n_vec)
+            BwdVec<T, kKind>::grad(x[q][j], dy[q][j], w[j], r[q], shift[q], c1, c2, out[q], lane + j * kLanes);
+      }
+    }
+  }
+  if (!a.want_grads) return;
+  // the teams of a block, added in their order
+  __shared__ float sum[kTeams][kLanes * kVecs * 8 + 1];
+  float* const part_w = a.part + static_cast<int64_t>(blockIdx.x) * a.dim;
+  float* const part_b = part_w + static_cast<int64_t>(gridDim.x) * a.dim;
+#pragma unroll
+  for (int pass = 0; pass < (kKind == kRms ? 1 : 2); ++pass) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum[team][(lane + j * kLanes) * 8 + k] = pass ? db[j][k] : dw[j][k];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.dim; c += 256) {
+      float total = 0.f;
+#pragma unroll 8
+      for (int t = 0; t < kTeams; ++t) total += sum[t][c];
+      (pass ? part_b : part_w)[c] = total;
+    }
+  }
+}
+
+// Long rows: a block a row, kVecs vectors a thread, kRows rows at a time, a.stages of these ahead
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <typename T, int kVecs, int kRows, int kKind>
+__global__ void __launch_bounds__(512) norm_bwd_long_kernel(const NormArgs a) {
+  constexpr int kParts = kRows * (kKind == kLayerBias ? 2 : 1), kVecBytes = 8 * static_cast<int>(sizeof(T));
+  extern __shared__ __align__(16) char ring[];  // [stages][rows][x, dy][threads * kVecs] vectors
+  __shared__ __align__(16) float part[2][kParts][16];
+  const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31;
+  const int n_vec = a.dim / 8, stages = a.stages;
+  const uint32_t row_bytes = static_cast<uint32_t>(threads) * kVecs * kVecBytes, stage_bytes = 2 * kRows * row_bytes;
+  float dw[kVecs][8], db[kVecs][8];
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[j][k] = 0.f, db[j][k] = 0.f;
+  }
+  for (int i = tid; i < 2 * kParts * 16; i += threads) (&part[0][0][0])[i] = 0.f;
+  grid_wait_predecessor();
+  grid_launch_dependents();
+  const uint32_t mine = smem_u32(ring) + tid * kVecBytes;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  // The copies of the rows base .. base + kRows - 1 (one group, empty behind the last row)
+  auto fetch = [&](int64_t base, int stage) {
+    const uint32_t to = mine + stage * stage_bytes;
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      if (base + q < a.rows) {
+        int64_t o;
+        int i;
+        row_of(static_cast<uint32_t>(base + q), a.inner, o, i);
+        const char *px = a.x.p + o * a.x.outer + i * a.x.inner, *pg = a.dy.p + o * a.dy.outer + i * a.dy.inner;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+          const int v = tid + j * threads;
+          if (v < n_vec) {
+#pragma unroll
+            for (int e = 0; e < kVecBytes; e += 16) {
+              copy_async16(to + (2 * q) * row_bytes + j * threads * kVecBytes + e, px + static_cast<int64_t>(v) * kVecBytes + e);
+              copy_async16(to + (2 * q + 1) * row_bytes + j * threads * kVecBytes + e, pg + static_cast<int64_t>(v) * kVecBytes + e);
+            }
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int64_t base = static_cast<int64_t>(blockIdx.x) * kRows, ahead = base;
+  for (int i = 0; i < stages; ++i, ahead += step) fetch(ahead, i);
+  __syncthreads();
+  int turn = 0;
+  for (int stage = 0; base < a.rows; base += step, ahead += step, turn ^= 1) {
+    if (stages >= 3)
+      asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 2)
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    Vec<T, 8> x[kRows][kVecs], dy[kRows][kVecs];
+    float r[kRows], shift[kRows], sum[kParts];
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      const bool here = base + q < a.rows;
+      r[q] = here ? __ldg(a.rstd + base + q) : 0.f;
+      shift[q] = kKind == kLayerBias && here ? -__ldg(a.mean + base + q) : 0.f;
+      const char* from = ring + static_cast<size_t>(stage) * stage_bytes + tid * kVecBytes + 2 * q * row_bytes;
+      float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+        const int v = tid + j * threads;
+        if (here && v < n_vec) {
+          x[q][j].load(from, j * threads), dy[q][j].load(from + row_bytes, j * threads);
+          float w[8];
+          load_params<8>(a.w, a.w_f32, v * 8, 1.f, w);
+          BwdVec<T, kKind>::sums(x[q][j], dy[q][j], w, r[q], shift[q], s, c, dw[j], db[j]);
+        }
+      }
+      sum[q] = s[0] + s[1];
+      if (kKind == kLayerBias) sum[kRows + q] = c[0] + c[1];
+    }
+    fetch(ahead, stage);  // over what this thread has just read
+    if (++stage == stages) stage = 0;
+    const float one = lanes_sum<kParts, 32>(sum, lane);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+      if (lane == sum_at<kParts, 32>(k)) part[turn][k][warp] = one;
+    __syncthreads();  // the other set is written behind the next barrier but one at the earliest
+    float total[kParts];
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      float4 f = *reinterpret_cast<const float4*>(part[turn][k]);
+      float t0 = f.x + f.z, t1 = f.y + f.w;
+      for (int i = 4; i < threads >> 5; i += 4) {
+        f = *reinterpret_cast<const float4*>(part[turn][k] + i);
+        t0 += f.x + f.z, t1 += f.y + f.w;
+      }
+      total[k] = (t0 + t1) * a.inv_dim;
+    }
+#pragma unroll
+    for (int q = 0; q < kRows; ++q) {
+      if (base + q < a.rows) {
+        int64_t o;
+        int i;
+        row_of(static_cast<uint32_t>(base + q), a.inner, o, i);
+        char* out = a.y.p + o * a.y.outer + i * a.y.inner;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+          const int v = tid + j * threads;
+          if (v < n_vec) {
+            float w[8];
+            load_params<8>(a.w, a.w_f32, v * 8, 1.f, w);
+            BwdVec<T, kKind>::grad(x[q][j], dy[q][j], w, r[q], shift[q], total[q], kKind == kLayerBias ? total[kRows + q] : 0.f, out, v);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!a.want_grads) return;
+  float* const part_w = a.part + static_cast<int64_t>(blockIdx.x) * a.dim;
+  float* const part_b = part_w + static_cast<int64_t>(gridDim.x) * a.dim;
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int v = tid + j * threads;
+    if (v < n_vec) {
+#pragma unroll
+      for (int k = 0; k < 8; k += 4) {
+        *reinterpret_cast<float4*>(part_w + v * 8 + k) = make_float4(dw[j][k], dw[j][k + 1], dw[j][k + 2], dw[j][k + 3]);
+        if (kKind != kRms) *reinterpret_cast<float4*>(part_b + v * 8 + k) = make_float4(db[j][k], db[j][k + 1], db[j][k + 2], db[j][k + 3]);
+      }
+    }
+  }
+}
+
+// dw and db (the second half of the blocks) from the sums of the blocks: 32 columns a block, a warp for every 32nd sum.
+__global__ void __launch_bounds__(1024) norm_grads_kernel(const float* part, int blocks, int dim, float* dw, float* db) {
+  __shared__ float sum[32][33];
   grid_wait_predecessor();
   grid_launch_dependents();
   const int half = static_cast<int>(gridDim.x) / 2, which = static_cast<int>(blockIdx.x) >= half;
-  const int c = (blockIdx.x - which * half) * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, c = (blockIdx.x - which * half) * 32 + lane;
   float* const out = which ? db : dw;
   if (!out) return;
   const float* p = part + static_cast<int64_t>(which) * blocks * dim + c;
   float total = 0.f;
   if (c < dim) {
 #pragma unroll 8
-    for (int i = k; i < blocks; i += 8) total += p[static_cast<int64_t>(i) * dim];
+    for (int i = k; i < blocks; i += 32) total += p[static_cast<int64_t>(i) * dim];
   }
-  sum[k][threadIdx.x & 31] = total;
+  sum[k][lane] = total;
   __syncthreads();
   if (k == 0 && c < dim) {
+    total = 0.f;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) total += sum[i][threadIdx.x];
+    for (int i = 0; i < 32; ++i) total += sum[i][lane];
     out[c] = total;
   }
 }
 
 constexpr int kSms = 148;
-constexpr int kTeamBlock = 256;
+constexpr int kMostShared = 227 * 1024;
 
-// How a row is divided: elements of a vector, threads of a team, vectors of a thread, blocks an SM (of the walk).
-struct Shape {
-  int vec, team, per, block;
-  bool whole;  // the team is the block
+// A launch: which kernel, blocks and threads, shared memory and stages of the long rows' kernel.
+struct Launch {
+  void (*kernel)(const NormArgs) = nullptr;
+  int64_t blocks = 0;
+  int threads = 0, shared = 0, stages = 0;
 };
-Shape shape_of(int dim, bool vectors, bool backward) {
-  Shape s{vectors ? 8 : 1, 0, 1, kTeamBlock, false};
-  const int n = dim / s.vec;
-  if (!vectors) {
-    s.per = 8;
-    if (n <= 256) {
-      s.team = 32;
-    } else {
-      if (n > 8192) s.per = 16;
-      s.team = s.block = ((n + s.per - 1) / s.per + 31) / 32 * 32, s.whole = true;
-    }
-    return s;
+
+int round32(int n) { return (n + 31) / 32 * 32; }
+
+// Rows element by element: up to 8 elements a lane of a warp, or up to 16 a thread of a block.
+template <typename T, bool kLayer>
+Launch element_launch(int dim, int64_t rows, bool backward) {
+  Launch l;
+  int teams = 1;
+  if (dim <= 256) {
+    l.kernel = backward ? norm_bwd_element_kernel<T, 1, 8, 32, kLayer> : norm_fwd_element_kernel<T, 1, 8, 32, kLayer>;
+    l.threads = 256, teams = 8;
+  } else if (dim <= 8192) {
+    l.kernel = backward ? norm_bwd_element_kernel<T, 1, 8, 0, kLayer> : norm_fwd_element_kernel<T, 1, 8, 0, kLayer>;
+    l.threads = round32((dim + 7) / 8);
+  } else {
+    l.kernel = backward ? norm_bwd_element_kernel<T, 1, 16, 0, kLayer> : norm_fwd_element_kernel<T, 1, 16, 0, kLayer>;
+    l.threads = round32((dim + 15) / 16);
   }
-  if (n <= 8) s.team = 8;
-  else if (n <= 16) s.team = 16;
-  else if (n <= 32) s.team = 32;
-  else if (n <= 64) s.team = 32, s.per = 2;
+  const int64_t need = (rows + teams - 1) / teams, most = kSms * (1024 / l.threads > 1 ? 1024 / l.threads : 1);
+  l.blocks = need < most ? need : most;
+  return l;
+}
+
+// Vectors a lane and warps a row in the forward pass: 128 bytes of registers a lane hold 16 vectors of bf16 or 8 of fp32.
+template <typename T, bool kLayer>
+Launch fwd_launch(int dim, int64_t rows) {
+  const int n = dim / 8;
+  Launch l;
+  int per_block = 0;
+  auto use = [&](void (*k)(const NormArgs), int lanes, int warps, int rows_of_team) {
+    l.kernel = k, l.threads = warps > 4 ? 32 * warps : 128, per_block = l.threads / (lanes * warps) * rows_of_team;
+  };
+  if (n <= 8) use(norm_fwd_kernel<T, 8, 1, 1, 4, kLayer>, 8, 1, 4);
+  else if (n <= 16) use(norm_fwd_kernel<T, 8, 2, 1, 2, kLayer>, 8, 1, 2);
+  else if (n <= 32) use(norm_fwd_kernel<T, 16, 2, 1, 2, kLayer>, 16, 1, 2);
+  else if (n <= 64) use(norm_fwd_kernel<T, 32, 2, 1, 2, kLayer>, 32, 1, 2);
+  else if (n <= 128) use(norm_fwd_kernel<T, 32, 4, 1, 1, kLayer>, 32, 1, 1);
+  else if (n <= 256) use(norm_fwd_kernel<T, 32, 8, 1, 1, kLayer>, 32, 1, 1);
+  else if constexpr (sizeof(T) == 2) {
+    if (n <= 512) use(norm_fwd_kernel<T, 32, 16, 1, 1, kLayer>, 32, 1, 1);
+    else if (n <= 1024) use(norm_fwd_kernel<T, 32, 16, 2, 1, kLayer>, 32, 2, 1);
+    else use(norm_fwd_kernel<T, 32, 16, 4, 1, kLayer>, 32, 4, 1);
+  } else {
+    if (n <= 512) use(norm_fwd_kernel<T, 32, 8, 2, 1, kLayer>, 32, 2, 1);
+    else if (n <= 1024) use(norm_fwd_kernel<T, 32, 8, 4, 1, kLayer>, 32, 4, 1);
+    else use(norm_fwd_kernel<T, 32, 8, 8, 1, kLayer>, 32, 8, 1);
+  }
+  l.blocks = (rows + per_block - 1) / per_block;
+  return l;
+}
+
+template <typename T, int kKind>
+Launch bwd_launch(int dim, int64_t rows) {
+  const int n = dim / 8;
+  Launch l;
+  int64_t most = 0;
+  int rows_of_block = 0;
+  auto brief = [&](void (*k)(const NormArgs), int lanes, int rows_of_team) {
+    l.kernel = k, l.threads = 256, rows_of_block = 256 / lanes * rows_of_team, most = 2 * kSms;
+  };
+  if (n <= 8) brief(norm_bwd_short_kernel<T, 8, 1, 4, kKind>, 8, 4);
+  else if (n <= 16) brief(norm_bwd_short_kernel<T, 8, 2, 2, kKind>, 8, 2);
+  else if (n <= 32) brief(norm_bwd_short_kernel<T, 16, 2, 2, kKind>, 16, 2);
+  else if (n <= 64) brief(norm_bwd_short_kernel<T, 32, 2, 2, kKind>, 32, 2);
   else {
-    s.whole = true;
-    s.per = backward ? (n <= 512 ? 1 : 2) : (n <= 256 ? 1 : n <= 512 ? 2 : 4);
-    s.team = s.block = ((n + s.per - 1) / s.per + 31) / 32 * 32;
+    int vecs = 2;
+    if (sizeof(T) == 2) {
+      rows_of_block = n <= 1024 ? 2 : 1;
+      if (n > 1024) vecs = 4, l.kernel = norm_bwd_long_kernel<T, 4, 1, kKind>;
+      else l.kernel = norm_bwd_long_kernel<T, 2, 2, kKind>;
+    } else {
+      rows_of_block = 1;
+      if (n > 1024) vecs = 4, l.kernel = norm_bwd_long_kernel<T, 4, 1, kKind>;
+      else l.kernel = norm_bwd_long_kernel<T, 2, 1, kKind>;
+    }
+    l.threads = round32((n + vecs - 1) / vecs);
+    const int stage = 2 * rows_of_block * l.threads * vecs * 8 * static_cast<int>(sizeof(T));
+    // two blocks an SM where three stages of each fit, or four of short ones
+    const int by_threads = 1024 / l.threads < 4 ? 1024 / l.threads : 4;
+    int per_sm = by_threads;
+    while (per_sm > 1 && per_sm * (3 * stage + 2048) > kMostShared) --per_sm;
+    l.stages = 3;
+    while (l.stages > 1 && l.stages * stage + 2048 > kMostShared) --l.stages;
+    l.shared = l.stages * stage;
+    most = static_cast<int64_t>(per_sm) * kSms;
   }
-  return s;
-}
-int blocks_of(const Shape& s, int64_t rows) {
-  const int64_t teams = s.block / s.team, need = (rows + teams - 1) / teams;
-  const int64_t most = kSms * (s.block >= 1024 ? 1 : 1024 / s.block);
-  return static_cast<int>(need < most ? need : most);
+  const int64_t need = (rows + rows_of_block - 1) / rows_of_block;
+  l.blocks = need < most ? need : most;
+  return l;
 }
 
-template <template <typename, int, int, int, bool> class K, typename T, bool kLayer>
-void (*pick(const Shape& s))(const NormArgs) {
-  if (s.vec == 1) {
-    if (!s.whole) return K<T, 1, 8, 32, kLayer>::fn();
-    return s.per == 8 ? K<T, 1, 8, 0, kLayer>::fn() : K<T, 1, 16, 0, kLayer>::fn();
+Launch launch_of(bool vectors, int dim, int64_t rows, int dtype, bool layer, bool bias, bool backward) {
+  const bool f32 = dtype == NSP_F32;
+  if (!vectors) {
+    if (f32) return layer ? element_launch<float, true>(dim, rows, backward) : element_launch<float, false>(dim, rows, backward);
+    return layer ? element_launch<__nv_bfloat16, true>(dim, rows, backward) : element_launch<__nv_bfloat16, false>(dim, rows, backward);
   }
-  if (!s.whole) {
-    if (s.per == 2) return K<T, 8, 2, 32, kLayer>::fn();
-    return s.team == 8 ? K<T, 8, 1, 8, kLayer>::fn() : s.team == 16 ? K<T, 8, 1, 16, kLayer>::fn() : K<T, 8, 1, 32, kLayer>::fn();
+  if (!backward) {
+    if (f32) return layer ? fwd_launch<float, true>(dim, rows) : fwd_launch<float, false>(dim, rows);
+    return layer ? fwd_launch<__nv_bfloat16, true>(dim, rows) : fwd_launch<__nv_bfloat16, false>(dim, rows);
   }
-  return s.per == 1 ? K<T, 8, 1, 0, kLayer>::fn() : s.per == 2 ? K<T, 8, 2, 0, kLayer>::fn() : K<T, 8, 4, 0, kLayer>::fn();
+  if (f32) return layer ? bwd_launch<float, kLayerBias>(dim, rows) : bias ? bwd_launch<float, kRmsBias>(dim, rows) : bwd_launch<float, kRms>(dim, rows);
+  return layer ? bwd_launch<__nv_bfloat16, kLayerBias>(dim, rows)
+               : bias ? bwd_launch<__nv_bfloat16, kRmsBias>(dim, rows) : bwd_launch<__nv_bfloat16, kRms>(dim, rows);
 }
-template <typename T, int V, int NV, int kTeam, bool kLayer>
-struct Fwd {
-  static auto fn() { return norm_fwd_kernel<T, V, NV, kTeam, kLayer>; }
-};
-template <typename T, int V, int NV, int kTeam, bool kLayer>
-struct Bwd {
-  static auto fn() { return norm_bwd_kernel<T, V, (V * NV > 16 ? 2 : NV), kTeam, kLayer>; }  // four vectors: forward only
-};
+
+cudaError_t launch(const Launch& l, NormArgs& a, cudaStream_t st) {
+  if (l.shared > 40 * 1024) {  // with what the kernel has of its own, more than the 48 KB of an ordinary launch
+    const cudaError_t e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.shared);
+    if (e != cudaSuccess) return cudaGetLastError(), e;
+  }
+  a.stages = l.stages;
+  nsp::count_launches(1);
+  return nsp::launch_chained_if(true, l.kernel, static_cast<unsigned>(l.blocks), l.threads, l.shared, st, a);
+}
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
@@ -476,22 +951,20 @@ extern "C" int nsp_norm_fwd(const nsp_rows_t* x, const void* weight, const void*
   a.w = weight, a.b = bias, a.mean = mean, a.rstd = rstd;
   a.rows = outer * inner, a.inner = inner, a.dim = dim, a.w_f32 = w_dtype == NSP_F32;
   a.eps = eps, a.inv_dim = 1.f / static_cast<float>(dim);
-  const Shape s = shape_of(dim, vectors, false);
-  const bool layer = kind == NSP_NORM_LAYER;
-  void (*kernel)(const NormArgs) = dtype == NSP_F32 ? (layer ? pick<Fwd, float, true>(s) : pick<Fwd, float, false>(s))
-                                                    : (layer ? pick<Fwd, __nv_bfloat16, true>(s) : pick<Fwd, __nv_bfloat16, false>(s));
-  nsp::count_launches(1);
-  return nsp::launch_chained_if(true, kernel, blocks_of(s, a.rows), s.block, 0, static_cast<cudaStream_t>(stream), a) == cudaSuccess
-             ? NSP_OK : NSP_ERR_CUDA;
+  return launch(launch_of(vectors, dim, a.rows, dtype, kind == NSP_NORM_LAYER, false, false), a, static_cast<cudaStream_t>(stream)) ==
+                 cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }
 
 extern "C" int nsp_norm_bwd_ws_bytes(int64_t rows, int32_t dim, size_t* bytes) {
   if (!bytes || rows < 0 || dim < 1) return NSP_ERR_INVALID_ARG;
   if (dim > NSP_NORM_MAX_DIM || rows > INT32_MAX) return NSP_ERR_UNSUPPORTED;
-  int most = 0;
-  for (bool vectors : {false, true}) {
-    const int n = blocks_of(shape_of(dim, vectors, true), rows);
-    most = n > most ? n : most;
+  int64_t most = 0;  // of any kernel for rows of that length
+  for (int dtype : {NSP_BF16, NSP_F32}) {
+    for (bool vectors : {false, true}) {
+      if (vectors && dim % 8) continue;
+      const int64_t n = launch_of(vectors, dim, rows, dtype, true, true, true).blocks;
+      most = n > most ? n : most;
+    }
   }
   *bytes = 2 * sizeof(float) * static_cast<size_t>(most) * dim;
   return NSP_OK;
@@ -517,18 +990,15 @@ extern "C" int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const voi
     if (rc == NSP_OK) rc = check_rows(dx, outer, inner, dim, size, true, &vectors, &a.y);
     if (rc != NSP_OK) return rc;
     if (!same_place(a.x, a.y) || !same_place(a.dy, a.y)) return NSP_ERR_INVALID_ARG;
-    const Shape s = shape_of(dim, vectors, true);
-    blocks = blocks_of(s, a.rows);
+    const Launch l = launch_of(vectors, dim, a.rows, dtype, layer, dbias != nullptr, true);
+    blocks = static_cast<int>(l.blocks);
     if (grads && (!ws || !aligned(ws, 16) || ws_bytes < 2 * sizeof(float) * static_cast<size_t>(blocks) * dim)) return NSP_ERR_WORKSPACE;
     a.w = weight, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd), a.part = static_cast<float*>(ws);
     a.inner = inner, a.dim = dim, a.w_f32 = w_dtype == NSP_F32, a.want_grads = grads, a.inv_dim = 1.f / static_cast<float>(dim);
-    void (*kernel)(const NormArgs) = dtype == NSP_F32 ? (layer ? pick<Bwd, float, true>(s) : pick<Bwd, float, false>(s))
-                                                      : (layer ? pick<Bwd, __nv_bfloat16, true>(s) : pick<Bwd, __nv_bfloat16, false>(s));
-    nsp::count_launches(1);
-    if (nsp::launch_chained_if(true, kernel, blocks, s.block, 0, st, a) != cudaSuccess) return NSP_ERR_CUDA;
+    if (launch(l, a, st) != cudaSuccess) return NSP_ERR_CUDA;
   }
   if (!grads) return NSP_OK;
   nsp::count_launches(1);
-  return nsp::launch_chained_if(true, norm_grads_kernel, 2 * ((dim + 31) / 32), 256, 0, st, static_cast<const float*>(ws), blocks, dim,
+  return nsp::launch_chained_if(true, norm_grads_kernel, 2 * ((dim + 31) / 32), 1024, 0, st, static_cast<const float*>(ws), blocks, dim,
                                 dweight, dbias) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }

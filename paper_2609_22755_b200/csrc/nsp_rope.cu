@@ -10,11 +10,12 @@
 // turn, 2^-32 of a turn apart, and sincospif takes it from there. The error is p * 2^-65 of a turn, for any p a batch can
 // have below the rounding of the cosine.
 //
-// Work. A thread owns V pairs of a head (one 16-byte load for each half of them in bf16) of up to four neighbouring heads of
-// one token: the sines and cosines are computed once for these, while the loads are under way. Groups of J threads, one per slot
-// of a head, cover all slots of a (token, heads) piece.
+// Work. A thread owns V pairs of a head (one 16-byte load for each half of them in bf16) of up to 16 neighbouring heads of one
+// token: the sines and cosines are computed once for these, and up to four heads' loads are under way at a time. Groups of J
+// threads, one per slot of a head, cover all slots of a (token, heads) piece.
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include "nsp_internal.cuh"
@@ -27,7 +28,7 @@ using nsp::pack_bf16x2;
 namespace {
 
 constexpr int kMaxPairs = NSP_ROPE_MAX_ROT / 2;
-constexpr int kMostHeads = 4;  // heads of a thread
+constexpr int kMostHeads = 16;  // heads of a thread
 
 struct RopeTensor {
   const void* x;
@@ -104,6 +105,7 @@ struct Raw {
 template <typename T, int V, bool kHalf>
 __device__ __forceinline__ void rope_piece(const RopeTensor& t, const uint64_t* freq, uint32_t token, int h0, int slot, int rot_slots,
                                            int dim, int rot, float magnitude, float sin_sign) {
+  constexpr int kBatch = V * sizeof(T) > 16 ? 2 : 4;  // heads whose loads are under way together
   const int n = min(t.per, t.heads - h0);
   const T* x = static_cast<const T*>(t.x) + static_cast<int64_t>(token) * t.x_tok + h0 * t.x_head;
   T* y = static_cast<T*>(t.y) + static_cast<int64_t>(token) * t.y_tok + h0 * t.y_head;
@@ -119,61 +121,61 @@ __device__ __forceinline__ void rope_piece(const RopeTensor& t, const uint64_t* 
     b_at = a_at + V;
     second = b_at < dim;
   }
-  Raw<T, V> a[kMostHeads], b[kMostHeads];
+  const uint64_t p = t.pos ? static_cast<uint64_t>(t.pos[token]) : token;
+  float c[V], s[V];
+  for (int first = 0; first < n; first += kBatch, x += kBatch * t.x_head, y += kBatch * t.y_head) {
+    Raw<T, V> a[kBatch], b[kBatch];
 #pragma unroll
-  for (int i = 0; i < kMostHeads; ++i) {
-    if (i < n) {
-      a[i].load(x + i * t.x_head + a_at);
-      if (second) b[i].load(x + i * t.x_head + b_at);
+    for (int i = 0; i < kBatch; ++i) {
+      if (first + i < n) {
+        a[i].load(x + i * t.x_head + a_at);
+        if (second) b[i].load(x + i * t.x_head + b_at);
+      }
     }
-  }
-  if (!rotates) {
+    if (rotates) {
+      if (first == 0) {
 #pragma unroll
-    for (int i = 0; i < kMostHeads; ++i) {
-      if (i < n) {
+        for (int i = 0; i < V; ++i) {
+          const int32_t turn = static_cast<int32_t>((p * freq[slot * V + i]) >> 32);
+          sincospif(static_cast<float>(turn) * 0x1p-31f, &s[i], &c[i]);
+          c[i] *= magnitude;
+          s[i] *= sin_sign;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        float u[V], v[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          // pair k of the slot; neighbours: elements 2 k and 2 k + 1 of the two vectors
+          const int e = 2 * k;
+          const float p0 = kHalf ? a[i].get(k) : (e < V ? a[i].get(e % V) : b[i].get(e % V));
+          const float p1 = kHalf ? b[i].get(k) : (e + 1 < V ? a[i].get((e + 1) % V) : b[i].get((e + 1) % V));
+          const float q0 = p0 * c[k] - p1 * s[k], q1 = p1 * c[k] + p0 * s[k];
+          if (kHalf) {
+            u[k] = q0, v[k] = q1;
+          } else {
+            (e < V ? u : v)[e % V] = q0;
+            (e + 1 < V ? u : v)[(e + 1) % V] = q1;
+          }
+        }
+        a[i].set(u);
+        b[i].set(v);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (first + i < n) {
         a[i].store(y + i * t.y_head + a_at);
         if (second) b[i].store(y + i * t.y_head + b_at);
       }
     }
-    return;
-  }
-  const uint64_t p = t.pos ? static_cast<uint64_t>(t.pos[token]) : token;
-  float c[V], s[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int32_t turn = static_cast<int32_t>((p * freq[slot * V + i]) >> 32);
-    sincospif(static_cast<float>(turn) * 0x1p-31f, &s[i], &c[i]);
-    c[i] *= magnitude;
-    s[i] *= sin_sign;
-  }
-#pragma unroll
-  for (int i = 0; i < kMostHeads; ++i) {
-    if (i < n) {
-      float u[V], v[V];
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        // pair k of the slot; neighbours: elements 2 k and 2 k + 1 of the two vectors
-        const int e = 2 * k;
-        const float p0 = kHalf ? a[i].get(k) : (e < V ? a[i].get(e % V) : b[i].get(e % V));
-        const float p1 = kHalf ? b[i].get(k) : (e + 1 < V ? a[i].get((e + 1) % V) : b[i].get((e + 1) % V));
-        const float q0 = p0 * c[k] - p1 * s[k], q1 = p1 * c[k] + p0 * s[k];
-        if (kHalf) {
-          u[k] = q0, v[k] = q1;
-        } else {
-          (e < V ? u : v)[e % V] = q0;
-          (e + 1 < V ? u : v)[(e + 1) % V] = q1;
-        }
-      }
-      a[i].set(u);
-      b[i].set(v);
-      a[i].store(y + i * t.y_head + a_at);
-      b[i].store(y + i * t.y_head + b_at);
-    }
   }
 }
 
-template <int V, bool kHalf>
-__global__ void __launch_bounds__(V == 1 ? 512 : 256) rope_kernel(const __grid_constant__ RopeArgs a) {
+// kF32: tensors of either type; otherwise all of them bf16
+template <int V, bool kHalf, bool kF32>
+__global__ void __launch_bounds__(V == 1 ? 512 : 256, V == 1 ? 1 : kF32 ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ uint64_t freq[kMaxPairs];
   for (int i = threadIdx.x; i < a.pairs; i += blockDim.x) freq[i] = a.freq[i];
   grid_wait_predecessor();
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 256) rope_kernel(const __grid_c
   if (group >= static_cast<int64_t>(t.tokens) * t.chunks) return;
   const uint32_t token = static_cast<uint32_t>(group) / static_cast<uint32_t>(t.chunks);  // groups of a tensor: below 2^32
   const int h0 = static_cast<int>(static_cast<uint32_t>(group) - token * t.chunks) * t.per;
-  if (t.f32)
+  if (kF32 && t.f32)
     rope_piece<float, V, kHalf>(t, freq, token, h0, slot, a.rot_slots, a.dim, a.rot, a.magnitude, a.sin_sign);
   else
     rope_piece<__nv_bfloat16, V, kHalf>(t, freq, token, h0, slot, a.rot_slots, a.dim, a.rot, a.magnitude, a.sin_sign);
@@ -259,7 +261,7 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
   int vec = 8;  // elements of a vector, as far as every tensor's addresses allow
   auto fits = [&](int v) { return a.pairs % v == 0 && rot_dim % v == 0 && head_dim % v == 0; };
   while (vec > 1 && !fits(vec)) vec = vec == 8 ? 4 : 1;
-  bool copies = false;
+  bool copies = false, any_f32 = false;
   int64_t pieces = 0;  // (token, head)
   a.n = 0;
   for (int i = 0; i < n_tensors; ++i) {
@@ -277,6 +279,7 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
     if (s.x == s.y && ((s.tokens > 1 && s.x_token_stride != s.y_token_stride) || (s.heads > 1 && s.x_head_stride != s.y_head_stride)))
       return NSP_ERR_INVALID_ARG;
     if (s.x != s.y) copies = true;
+    if (s.dtype == NSP_F32) any_f32 = true;
     auto ok = [&](int v) {
       const uintptr_t bytes = static_cast<uintptr_t>(v * size > 16 ? 16 : v * size);
       auto stride = [&](int64_t e, int64_t count) { return count <= 1 || (e * size) % static_cast<int64_t>(bytes) == 0; };
@@ -311,11 +314,14 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
     blocks += (static_cast<int64_t>(t.tokens) * t.chunks + a.per_block - 1) / a.per_block;
   }
   if (blocks > INT32_MAX) return NSP_ERR_UNSUPPORTED;
-  void (*kernel)(const RopeArgs) = nullptr;
   const bool half = layout == NSP_ROPE_HALF;
-  if (vec == 8) kernel = half ? rope_kernel<8, true> : rope_kernel<8, false>;
-  else if (vec == 4) kernel = half ? rope_kernel<4, true> : rope_kernel<4, false>;
-  else kernel = half ? rope_kernel<1, true> : rope_kernel<1, false>;
+  auto pick = [&](auto v) {
+    constexpr int V = decltype(v)::value;
+    return any_f32 ? (half ? rope_kernel<V, true, true> : rope_kernel<V, false, true>)
+                   : (half ? rope_kernel<V, true, false> : rope_kernel<V, false, false>);
+  };
+  void (*kernel)(const RopeArgs) = vec == 8 ? pick(std::integral_constant<int, 8>{})
+                                   : vec == 4 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 1>{});
   nsp::count_launches(1);
   return nsp::launch_chained_if(true, kernel, static_cast<unsigned>(blocks), a.slots * a.per_block, 0, static_cast<cudaStream_t>(stream),
                                 a) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
