@@ -6,15 +6,18 @@
 //               dWg = dg^T x, dWu = du^T x, dx = dg Wg + du Wu, all three in one launch
 // 4 T d f flop there and 8 T d f back: bound by the tensor cores from some hundred tokens on, below by the bytes of the weights.
 //
-// Products. A pair of CTAs (tcgen05 cta_group::2) computes tiles of 256 rows x 2 `nh` columns: each CTA loads its own 128 rows of A
+// Products. A pair of CTAs (tcgen05 cta_group::2) computes tiles of 256 or 512 rows x 2 `nh` columns: each CTA loads its own rows of A
 // and its own nh rows of B by TMA, so that a byte of either operand is staged once for the two SMs that use it. In the forward pass
 // the first CTA's part of B comes from Wg and the second one's from Wu. Operands whose contraction index is not the contiguous one
-// (dg^T, du^T, x, and the weights of dx) are read MN-major by the tensor core: nothing is transposed in memory. Accumulators in
-// TMEM are double-buffered: 256 columns of the next tile are filled while the epilogue drains the last one's.
-// A stage holds 128 steps of the contraction and is filled by two instructions, one a warp: a 3-D box is two blocks of 64 columns at
-// once. What bounded the kernel before was not the bytes but the number of TMA instructions one thread issues (16,384 tokens, 4,096
-// x 12,288: stages of 64 steps and boxes of 64 columns 2,700 us there and 7,000 back, boxes of 128 columns 2,670 and 5,790, stages
-// of 128 steps 2,390 and 4,840).
+// (dg^T, du^T, x, and the weights of dx) are read MN-major by the tensor core: nothing is transposed in memory.
+//   flat tiles, 256 rows: the accumulators in TMEM are double-buffered, 256 columns of the next tile are filled while the epilogue
+//     drains the last one's.
+//   tall tiles, 512 rows: two products share a stage of B, their accumulators fill TMEM, and the next tile's first products wait
+//     for the epilogue to read the first half; up to four stages of them are issued before the second half is needed. A quarter
+//     less to load for the same products.
+// A stage of an operand is one instruction of one warp: a 3-D box is several blocks of 64 columns at once. With stages of 64 steps
+// and boxes of 64 columns the kernel was bound by the number of TMA instructions a thread issues (16,384 tokens, 4,096 x 12,288: 2,700
+// us there and 7,000 back; boxes of 128 columns 2,670 and 5,790; stages of 128 steps 2,390 and 4,840).
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -26,12 +29,21 @@
 namespace nsp {
 namespace {
 
-constexpr int kStages = 3;
-constexpr int kDepth = 128;                       // steps of the contraction in a stage
-constexpr uint32_t kBlock = 128 * 64 * 2;         // bytes of a block of 128 rows x 64 columns
-constexpr uint32_t kOperand = 128 * kDepth * 2;
-constexpr int kThreads = 384;                     // producer of A, issuer, producer of B, an idle warp, two warpgroups of epilogue
-constexpr int kGroupM = 8;                        // row tiles that are walked together (see tile_at)
+// A stage: kDepth steps of the contraction, of kRows rows of A and up to 128 of B.
+template <bool kTall>
+struct Geometry {
+  static constexpr int kDepth = kTall ? 64 : 128, kStages = kTall ? 4 : 3;
+  static constexpr int kHalves = kTall ? 2 : 1;  // products of 256 rows a stage of B is used for
+  static constexpr int kRows = 128 * kHalves;
+  static constexpr uint32_t kBytesA = kRows * kDepth * 2, kBytesB = 128 * kDepth * 2;
+  static constexpr uint32_t kBlockMn = kDepth * 128;  // bytes of 64 columns of an MN-major operand
+};
+constexpr uint32_t kOperands = 3 * 64 * 1024;
+static_assert(Geometry<true>::kStages * (Geometry<true>::kBytesA + Geometry<true>::kBytesB) == kOperands, "stages");
+static_assert(Geometry<false>::kStages * (Geometry<false>::kBytesA + Geometry<false>::kBytesB) == kOperands, "stages");
+constexpr uint32_t kBlock = 128 * 64 * 2;  // bytes of a block of 128 rows x 64 columns
+constexpr int kThreads = 384;              // producer of A, issuer, producer of B, an idle warp, two warpgroups of epilogue
+constexpr int kGroupM = 8, kGroupTall = 4; // row tiles that are walked together (see tile_at)
 constexpr long long kWaitLimit = NSP_WAIT_CYCLES_DEFAULT;
 constexpr int kMostMaps = 20, kMostProblems = 3;
 
@@ -80,13 +92,12 @@ struct Maps {
 };
 
 struct Smem {
-  uint8_t a[kStages][kOperand];
-  uint8_t b[kStages][kOperand];
-  uint8_t out[2][kBlock];    // a warpgroup's block of an output on its way to memory
-  uint64_t full[kStages];    // in the first CTA: the bytes of both
-  uint64_t empty[kStages];   // in both: the products of the stage have completed
-  uint64_t acc_full[2];      // in both: an accumulator is complete
-  uint64_t acc_empty[2];     // in the first CTA: 16 warps have read it
+  uint8_t operands[kOperands];  // stages of A, then of B
+  uint8_t out[2][kBlock];       // a warpgroup's block of an output on its way to memory
+  uint64_t full[4];             // in the first CTA: the bytes of both
+  uint64_t empty[4];            // in both: the products of the stage have completed
+  uint64_t acc_full[2];         // in both: an accumulator is complete (tall tiles: both halves, the first barrier)
+  uint64_t acc_empty[2];        // in the first CTA: 16 warps have read it
   uint32_t tmem_base;
   int32_t abort;
 };
@@ -115,11 +126,12 @@ __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
   }
 }
 
-// The tiles of a problem: kGroupM row tiles at a time, over all column tiles, so that the tiles under way at one time share
+// The tiles of a problem: kGroup row tiles at a time, over all column tiles, so that the tiles under way at one time share
 // both their rows and their columns in L2.
+template <int kGroup>
 __device__ __forceinline__ void tile_at(const Problem& p, int tile, int& m, int& n) {
-  const int per_group = kGroupM * p.tiles_n, group = tile / per_group, rest = tile - group * per_group;
-  const int first = group * kGroupM, size = min(kGroupM, p.tiles_m - first);
+  const int per_group = kGroup * p.tiles_n, group = tile / per_group, rest = tile - group * per_group;
+  const int first = group * kGroup, size = min(kGroup, p.tiles_m - first);
   n = rest / size;
   m = first + rest - n * size;
 }
@@ -140,19 +152,21 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* smem_
 // One operand of a stage. `across` is the index of its rows (columns of the output for B), `k` the step of the contraction, `wide`
 // the rows of this CTA. maps[0] holds whole blocks of 64 contiguous columns, two of them a box: {64, the other index, blocks};
 // maps[1] is the plain matrix, for boxes that the end of the contiguous index cuts: the rest reads as zero.
+template <int kDepth>
 __device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* maps, uint32_t bar, int mn, int across, int k, int wide,
                                              int across_end, int k_end) {
   const int at = mn ? across : k, other = mn ? k : across, end = mn ? across_end : k_end, cols = mn ? wide : kDepth;
   if (at + cols <= end) {
     tma_load_3d_pair(dst, maps, bar, 0, other, at / 64);
   } else {
-    const uint32_t block = mn ? kBlock : static_cast<uint32_t>(wide) * 128;
+    const uint32_t block = (mn ? kDepth : wide) * 128;
     const int last = mn ? cols : min(cols, end - at);  // the contraction ends in this stage: no blocks behind it
     for (int c = 0; c < last; c += 64) tma_load_2d_pair(dst + c / 64 * block, maps + 1, bar, at + c, other);
   }
 }
+template <int kDepth>
 __device__ __forceinline__ uint32_t operand_bytes(int mn, int wide, int k, int k_end) {
-  return mn || k + 64 < k_end ? wide * kDepth * 2 : wide * kDepth;
+  return mn || k + 64 < k_end ? wide * kDepth * 2 : wide * 64 * 2;
 }
 
 // 32 columns of one row
@@ -170,6 +184,17 @@ struct BlockOut {
   uint8_t* stage;
   int wg, thread;
   __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+  __device__ __forceinline__ bool all(bool here) const {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred q, %2, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(static_cast<uint32_t>(here)), "r"(1 + wg)
+        : "memory");
+    return r != 0;
+  }
   __device__ __forceinline__ void begin() const {  // the block before has been read
     if (thread == 0) tma_store_wait_read();
     sync();
@@ -196,14 +221,16 @@ __device__ __forceinline__ void pack_row(const uint32_t (&r)[32], uint32_t (&w)[
 }
 
 // kAct < 0: the accumulator is the output; otherwise the forward pass with that activation
-template <int kAct>
+template <int kAct, bool kTall>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
+  using G = Geometry<kTall>;
+  constexpr int kDepth = G::kDepth, kStages = G::kStages, kTileRows = 2 * G::kRows, kGroup = kTall ? kGroupTall : kGroupM;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&s.acc_full[i], 1), mbar_init(&s.acc_empty[i], 16);
     s.abort = 0;
     fence_mbar_init();
@@ -230,6 +257,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
   }
   const int pairs = static_cast<int>(gridDim.x) / 2, pair = static_cast<int>(blockIdx.x) / 2;
   const int nh = a.nh;
+  auto stage_a = [&](uint32_t st) { return s.operands + st * G::kBytesA; };
+  auto stage_b = [&](uint32_t st) { return s.operands + kStages * G::kBytesA + st * G::kBytesB; };
   auto problem_of = [&](int tile) -> const Problem& {
     int k = 0;
     while (k + 1 < a.n_problems && tile >= a.p[k + 1].first_tile) ++k;
@@ -245,10 +274,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       for (int i = 0, tile; ok && (tile = a.order.tile(i, pair, pairs)) >= 0; ++i) {
         const Problem& p = problem_of(tile);
         int m, n;
-        tile_at(p, tile - p.first_tile, m, n);
+        tile_at<kGroup>(p, tile - p.first_tile, m, n);
         const int mine = static_cast<int>(rank);
-        const int across = is_a ? m * 256 + mine * 128 : p.b_shared ? n * 2 * nh + mine * nh : n * nh;
-        const int mn = is_a ? p.a_mn : p.b_mn, wide = is_a ? 128 : nh, end = is_a ? p.rows : p.cols;
+        const int across = is_a ? m * kTileRows + mine * G::kRows : p.b_shared ? n * 2 * nh + mine * nh : n * nh;
+        const int mn = is_a ? p.a_mn : p.b_mn, wide = is_a ? G::kRows : nh, end = is_a ? p.rows : p.cols;
         for (int seg = 0; seg < p.segments && ok; ++seg) {
           const CUtensorMap* map = &maps.m[is_a ? p.a_map[seg] : p.b_map[seg][mine]];
           for (int k = 0; k < p.k_iters; ++k, ++it) {
@@ -260,8 +289,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
               break;
             }
             if (is_a && rank == 0)
-              mbar_expect_tx(&s.full[st], 2 * (operand_bytes(p.a_mn, 128, k * kDepth, p.depth) + operand_bytes(p.b_mn, nh, k * kDepth, p.depth)));
-            load_operand(is_a ? s.a[st] : s.b[st], map, lead + off(&s.full[st]), mn, across, k * kDepth, wide, end, p.depth);
+              mbar_expect_tx(&s.full[st], 2 * (operand_bytes<kDepth>(p.a_mn, G::kRows, k * kDepth, p.depth) +
+                                               operand_bytes<kDepth>(p.b_mn, nh, k * kDepth, p.depth)));
+            load_operand<kDepth>(is_a ? stage_a(st) : stage_b(st), map, lead + off(&s.full[st]), mn, across, k * kDepth, wide, end, p.depth);
           }
         }
       }
@@ -275,42 +305,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     bool ok = true;
     for (int tile; ok && (tile = a.order.tile(static_cast<int>(n_done), pair, pairs)) >= 0; ++n_done) {
       const Problem& p = problem_of(tile);
-      const uint32_t buf = n_done & 1, d = buf * 256;
+      const uint32_t buf = kTall ? 0 : n_done & 1, turn = kTall ? n_done & 1 : (n_done >> 1) & 1;
       const uint32_t idesc = make_idesc_bf16(256, 2 * nh, p.a_mn, p.b_mn);
       // 16 steps of the contraction: 32 bytes of a row (four of them in a block), or 16 rows
-      const uint32_t a_lbo = p.a_mn ? (kBlock >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : kBlock >> 4;
-      const uint32_t b_lbo = p.b_mn ? (kBlock >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
-      bool here = cluster_wait_tmem(&s.acc_empty[buf], ((n_done >> 1) & 1) ^ 1, kWaitLimit);
-      if (!__all_sync(0xffffffffu, here)) {
-        if (lane == 0) report_timeout(a.status, tile, kWhereGluAccEmpty, 0), raise_abort();
-        break;
-      }
-      tc_fence_after_sync();
+      const uint32_t a_lbo = p.a_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : G::kRows * 8;
+      const uint32_t b_lbo = p.b_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
       const int iters = p.segments * p.k_iters;
-      for (int k = 0; k < iters; ++k, ++it) {
-        const uint32_t st = it % kStages, ph = (it / kStages) & 1;
-        here = *abort_flag == 0 && cluster_wait(&s.full[st], ph, kWaitLimit);
+      auto acc_free = [&](uint32_t which) -> bool {
+        const bool here = cluster_wait_tmem(&s.acc_empty[which], turn ^ 1, kWaitLimit);
+        if (!__all_sync(0xffffffffu, here)) {
+          if (lane == 0) report_timeout(a.status, tile, kWhereGluAccEmpty, static_cast<int32_t>(which)), raise_abort();
+          return false;
+        }
+        tc_fence_after_sync();
+        return true;
+      };
+      auto arrived = [&](int k) -> bool {
+        const uint32_t at = it + k;
+        const bool here = *abort_flag == 0 && cluster_wait(&s.full[at % kStages], (at / kStages) & 1, kWaitLimit);
         if (!__all_sync(0xffffffffu, here)) {
           if (lane == 0 && !*abort_flag) report_timeout(a.status, tile, kWhereGluFull, k);
           if (lane == 0) raise_abort();
-          ok = false;
-          break;
+          return false;
         }
         tc_fence_after_sync();
+        return true;
+      };
+      auto issue = [&](int k, uint32_t half, bool last_use) {
+        const uint32_t st = (it + k) % kStages;
         const int left = p.depth - (k >= p.k_iters ? k - p.k_iters : k) * kDepth;  // steps of the segment from this stage on
         if (leader) {
-          const uint32_t a_lo = smem_desc_addr(s.a[st]) | a_lbo, b_lo = smem_desc_addr(s.b[st]) | b_lbo;
+          const uint32_t a_lo = (smem_desc_addr(stage_a(st)) + half * (kBlock >> 4)) | a_lbo, b_lo = smem_desc_addr(stage_b(st)) | b_lbo;
 #pragma unroll
           for (int kk = 0; kk < kDepth / 16; ++kk) {
             if (kk * 16 < left)
-              umma2_ss_lh(d, a_lo + (kk >> 2) * a_next + (kk & 3) * a_step, hi, b_lo + (kk >> 2) * b_next + (kk & 3) * b_step, hi, idesc,
-                          (k | kk) != 0);
+              umma2_ss_lh((buf + half) * 256, a_lo + (kk >> 2) * a_next + (kk & 3) * a_step, hi, b_lo + (kk >> 2) * b_next + (kk & 3) * b_step,
+                          hi, idesc, (k | kk) != 0);
           }
-          umma2_commit(&s.empty[st]);
-          if (k + 1 == iters) umma2_commit(&s.acc_full[buf]);
+          if (last_use) umma2_commit(&s.empty[st]);
+          if (last_use && k + 1 == iters) umma2_commit(&s.acc_full[buf]);
         }
         __syncwarp();
+      };
+      ok = acc_free(buf);
+      int k = 0;
+      if constexpr (kTall) {
+        const int lead_in = min(kStages, iters);
+        for (; ok && k < lead_in; ++k) {
+          ok = arrived(k);
+          if (ok) issue(k, 0, false);
+        }
+        ok = ok && acc_free(1);
+        if (ok) {
+          for (k = 0; k < lead_in; ++k) issue(k, 1, true);
+        }
       }
+      for (; ok && k < iters; ++k) {
+        ok = arrived(k);
+        if (!ok) break;
+        issue(k, 0, !kTall);
+        if constexpr (kTall) issue(k, 1, true);
+      }
+      it += iters;
     }
   } else if (warp >= 4) {
     // ================================================================ epilogue: a warpgroup has half of the columns
@@ -320,18 +376,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     for (int tile; (tile = a.order.tile(static_cast<int>(n_done), pair, pairs)) >= 0; ++n_done) {
       const Problem& p = problem_of(tile);
       int m, n;
-      tile_at(p, tile - p.first_tile, m, n);
-      const uint32_t buf = n_done & 1;
-      const bool here = *abort_flag == 0 && mbar_wait(&s.acc_full[buf], (n_done >> 1) & 1, kWaitLimit);
-      if (!__all_sync(0xffffffffu, here)) {
-        if (lane == 0 && !*abort_flag) report_timeout(a.status, tile, kWhereGluAccFull, 0);
+      tile_at<kGroup>(p, tile - p.first_tile, m, n);
+      const uint32_t buf0 = kTall ? 0 : n_done & 1, turn = kTall ? n_done & 1 : (n_done >> 1) & 1;
+      const bool here = *abort_flag == 0 && mbar_wait(&s.acc_full[buf0], turn, kWaitLimit);
+      const int thread = quad * 32 + lane;
+      const BlockOut out{s.out[half], half, thread};
+      if (!out.all(here)) {  // the warpgroup goes on together: it meets at barriers below
+        if (lane == 0 && !here && !*abort_flag) report_timeout(a.status, tile, kWhereGluAccFull, 0);
         if (lane == 0) raise_abort();
         break;
       }
       tc_fence_after_sync();
-      const int row0 = m * 256 + static_cast<int>(rank) * 128, thread = quad * 32 + lane, row = row0 + thread;
+#pragma unroll 1
+      for (int j = 0; j < G::kHalves; ++j) {
+      const uint32_t buf = buf0 + j;
+      const int row0 = m * kTileRows + static_cast<int>(rank) * G::kRows + j * 128, row = row0 + thread;
       const uint32_t t0 = buf * 256 + lanes;
-      const BlockOut out{s.out[half], half, thread};
       auto drained = [&]() {  // this warp has read its part of the accumulator
         tc_fence_before_sync();
         __syncwarp();
@@ -404,6 +464,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
           }
           out.end(&maps.m[p.out_map], n * 2 * nh + half * nh + c, row0, p);
         }
+      }
       }
     }
     if (lane == 0) tma_store_wait();
@@ -508,9 +569,10 @@ bool encode_plain(CUtensorMap* out, const void* base, int64_t cols, int64_t rows
   const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
   return encode(out, base, 2, dims, strides, box);
 }
-// The two maps of an operand (see load_operand): boxes of `blocks` blocks of 64 columns, and the plain matrix. The first one
-// covers whole blocks alone, so that no box of it reads past the end of a row.
-bool encode_operand(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_rows, int blocks) {
+// The two maps of an operand (see load_operand): boxes of `box_rows` rows and several blocks of 64 columns, and the plain matrix.
+// The first one covers whole blocks alone, so that no box of it reads past the end of a row.
+bool encode_operand(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_rows, int box_cols) {
+  const int blocks = box_cols / 64;
   const cuuint64_t dims[3] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols < 64 ? 1 : cols / 64)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, 128};
   const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(blocks)};
@@ -522,8 +584,9 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 // The order of n_long tiles of `cost` stages and n_short of `less` <= cost for that many pairs: `ahead` and `start` of the smallest
 // latest end. (4,099 tokens, 2,056 x 5,512 backward: 153 tiles of 88 stages and 396 of 33; the latest pair has 429 stages where all
 // tiles are dealt out one by one, 374 so, of a mean of 359.)
-Schedule plan_schedule(int n_long, int cost, int n_short, int less, int pairs) {
+Schedule plan_schedule(int n_long, int cost, int n_short, int less, int pairs, int64_t* latest) {
   Schedule best{n_long, n_short, n_long % pairs, 0, 0};
+  *latest = static_cast<int64_t>((n_long + pairs - 1) / pairs) * cost;
   if (n_short == 0) return best;
   int64_t best_end = -1;
   const int most = best.heavy ? (cost + less - 1) / less : 0;
@@ -546,17 +609,27 @@ Schedule plan_schedule(int n_long, int cost, int n_short, int less, int pairs) {
       if (best_end < 0 || end < best_end) best = s, best_end = end;
     }
   }
+  *latest = best_end;
   return best;
 }
 
 template <int kAct>
-cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, int pairs, cudaStream_t st) {
+cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, bool tall, int pairs, cudaStream_t st) {
   static_assert(sizeof(Maps) + sizeof(GemmArgs) <= 4000, "kernel parameters");
-  const cudaError_t e = cudaFuncSetAttribute(glu_gemm_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Smem)));
+  void (*kernel)(const Maps, const GemmArgs) = tall ? glu_gemm_kernel<kAct, true> : glu_gemm_kernel<kAct, false>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Smem)));
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_chained_if(true, glu_gemm_kernel<kAct>, 2 * pairs, kThreads, sizeof(Smem), st, maps, a);
+  return launch_chained_if(true, kernel, 2 * pairs, kThreads, sizeof(Smem), st, maps, a);
 }
+
+// Sizes of a launch's tiles.
+struct Tiling {
+  bool tall;
+  int rows, depth, pairs;  // rows of a tile, steps of a stage
+  Schedule order;
+};
+Tiling tiling(bool tall) { return Tiling{tall, tall ? 512 : 256, tall ? Geometry<true>::kDepth : Geometry<false>::kDepth, 0, {}}; }
 
 // A matrix of `rows` rows: address and row stride a TMA copy can take, and rows that do not overlap
 int check(const nsp_matrix_t* t, int64_t rows, int64_t cols) {
@@ -566,6 +639,16 @@ int check(const nsp_matrix_t* t, int64_t rows, int64_t cols) {
   return NSP_OK;
 }
 int64_t ld_of(const nsp_matrix_t* t, int64_t rows, int64_t cols) { return rows > 1 ? t->row_stride : cols; }
+
+// Tall tiles where they end the launch earlier, a tall one taken as kTallCost of two flat ones. latest(t) plans the order for t and
+// says how many steps of the contraction the pair with most of them has.
+constexpr double kTallCost = 0.95;
+template <typename F>
+Tiling choose_tiling(F latest) {
+  Tiling flat = tiling(false), tall = tiling(true);
+  const int64_t end_flat = latest(flat), end_tall = latest(tall);
+  return 2 * kTallCost * end_tall <= end_flat ? tall : flat;
+}
 
 int check_sizes(int64_t rows, int32_t d_model, int32_t d_ff, int32_t act) {
   if (rows < 0 || d_model < 1 || d_ff < 1 || (act != NSP_ACT_SILU && act != NSP_ACT_GELU)) return NSP_ERR_INVALID_ARG;
@@ -594,8 +677,16 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
   Maps maps;
   a.nh = 128;
   Problem& p = a.p[0];
-  p.tiles_m = ceil_div(T, 256), p.tiles_n = ceil_div(d_ff, a.nh);
-  p.segments = 1, p.depth = d_model, p.k_iters = ceil_div(d_model, kDepth);
+  p.tiles_n = ceil_div(d_ff, a.nh);
+  const Tiling t = choose_tiling([&](Tiling& t) {
+    const int n = ceil_div(T, t.rows) * p.tiles_n;
+    t.pairs = n < rec->sms / 2 ? n : rec->sms / 2;
+    int64_t latest;
+    t.order = plan_schedule(n, ceil_div(d_model, t.depth) * t.depth, 0, 0, t.pairs, &latest);
+    return latest;
+  });
+  p.tiles_m = ceil_div(T, t.rows);
+  p.segments = 1, p.depth = d_model, p.k_iters = ceil_div(d_model, t.depth);
   p.a_map[0] = 0, p.b_map[0][0] = 2, p.b_map[0][1] = 4, p.out_map = 6;
   p.rows = T, p.cols = d_ff;
   const nsp_matrix_t* outs[3] = {h, g, u};
@@ -605,16 +696,15 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
     p.ld[i] = ld_of(outs[i], rows, d_ff);
     if (!encode_plain(&maps.m[p.out_map + i], outs[i]->data, d_ff, rows, p.ld[i], 128)) return NSP_ERR_CUDA;
   }
-  if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), 128, 2) ||
-      !encode_operand(&maps.m[2], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), a.nh, 2) ||
-      !encode_operand(&maps.m[4], w_up->data, d_model, d_ff, ld_of(w_up, d_ff, d_model), a.nh, 2))
+  if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), t.rows / 2, t.depth) ||
+      !encode_operand(&maps.m[2], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), a.nh, t.depth) ||
+      !encode_operand(&maps.m[4], w_up->data, d_model, d_ff, ld_of(w_up, d_ff, d_model), a.nh, t.depth))
     return NSP_ERR_CUDA;
   a.n_problems = 1;
-  const int n_tiles = p.tiles_m * p.tiles_n, pairs = n_tiles < rec->sms / 2 ? n_tiles : rec->sms / 2;
-  a.order = plan_schedule(n_tiles, p.k_iters, 0, 0, pairs);
+  a.order = t.order;
   a.status = rec->word;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return (act == NSP_ACT_SILU ? launch_gemm<kSilu>(maps, a, pairs, st) : launch_gemm<kGelu>(maps, a, pairs, st)) == cudaSuccess
+  return (act == NSP_ACT_SILU ? launch_gemm<kSilu>(maps, a, t.tall, t.pairs, st) : launch_gemm<kGelu>(maps, a, t.tall, t.pairs, st)) == cudaSuccess
              ? NSP_OK : NSP_ERR_CUDA;
 }
 
@@ -663,49 +753,57 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   a.nh = 128;
   bool ok = true;
   // dg, du as [rows, d_ff]: the contraction of dx runs along their rows, that of the weights' gradients along their columns
-  int n_tiles = 0, tiles[2] = {0, 0}, cost[2] = {ceil_div(T, kDepth), 2 * ceil_div(d_ff, kDepth)};  // of dW, dx
-  auto add = [&](int cls, int64_t out_rows) -> Problem& {
+  const int tiles_n = ceil_div(d_model, 2 * a.nh);
+  const bool x_first = want_x && 2 * int64_t{d_ff} > rows;  // the longer tiles
+  const Tiling t = choose_tiling([&](Tiling& t) {
+    const int w_tiles = want_w ? 2 * ceil_div(d_ff, t.rows) * tiles_n : 0, x_tiles = want_x ? ceil_div(T, t.rows) * tiles_n : 0;
+    const int w_cost = ceil_div(T, t.depth) * t.depth, x_cost = 2 * ceil_div(d_ff, t.depth) * t.depth;
+    t.pairs = w_tiles + x_tiles < rec->sms / 2 ? w_tiles + x_tiles : rec->sms / 2;
+    int64_t latest;
+    t.order = x_first ? plan_schedule(x_tiles, x_cost, w_tiles, w_cost, t.pairs, &latest) : plan_schedule(w_tiles, w_cost, x_tiles, x_cost, t.pairs, &latest);
+    return latest;
+  });
+  int n_tiles = 0;
+  auto add = [&](int64_t out_rows) -> Problem& {
     Problem& p = a.p[a.n_problems++];
-    p.tiles_m = ceil_div(out_rows, 256), p.tiles_n = ceil_div(d_model, 2 * a.nh), p.first_tile = n_tiles;
+    p.tiles_m = ceil_div(out_rows, t.rows), p.tiles_n = tiles_n, p.first_tile = n_tiles;
     p.rows = static_cast<int32_t>(out_rows), p.cols = d_model, p.b_mn = p.b_shared = 1;
-    n_tiles += p.tiles_m * p.tiles_n, tiles[cls] += p.tiles_m * p.tiles_n;
+    n_tiles += p.tiles_m * p.tiles_n;
     return p;
   };
   auto add_w = [&]() {
     const nsp_matrix_t* outs[2] = {dw_gate, dw_up};
     for (int i = 0; i < 2; ++i) {
-      Problem& p = add(0, d_ff);
-      p.segments = 1, p.depth = T, p.k_iters = ceil_div(T, kDepth), p.a_mn = 1;
+      Problem& p = add(d_ff);
+      p.segments = 1, p.depth = T, p.k_iters = ceil_div(T, t.depth), p.a_mn = 1;
       p.a_map[0] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = 4, p.out_map = 14 + i;
-      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, kDepth, 2) &&
+      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.depth, t.rows / 2) &&
            encode_plain(&maps.m[14 + i], outs[i]->data, d_model, d_ff, ld_of(outs[i], d_ff, d_model), 128);
     }
-    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), kDepth, a.nh / 64);
+    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), t.depth, a.nh);
   };
   auto add_x = [&]() {
-    Problem& p = add(1, rows);
-    p.segments = 2, p.depth = d_ff, p.k_iters = ceil_div(d_ff, kDepth), p.out_map = 16;
+    Problem& p = add(rows);
+    p.segments = 2, p.depth = d_ff, p.k_iters = ceil_div(d_ff, t.depth), p.out_map = 16;
     ok = ok && encode_plain(&maps.m[16], dx->data, d_model, rows, ld_of(dx, rows, d_model), 128);
     for (int i = 0; i < 2; ++i) {
       const nsp_matrix_t* w = i ? w_up : w_gate;
       p.a_map[i] = 6 + 2 * i, p.b_map[i][0] = p.b_map[i][1] = 10 + 2 * i;
-      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, 128, 2) &&
-           encode_operand(&maps.m[10 + 2 * i], w->data, d_model, d_ff, ld_of(w, d_ff, d_model), kDepth, a.nh / 64);
+      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.rows / 2, t.depth) &&
+           encode_operand(&maps.m[10 + 2 * i], w->data, d_model, d_ff, ld_of(w, d_ff, d_model), t.depth, a.nh);
     }
   };
-  const int first = cost[1] > cost[0] && want_x ? 1 : 0;  // the class of the longer tiles
-  if (first == 1) add_x();
+  if (x_first) add_x();
   if (want_w) add_w();
-  if (first == 0 && want_x) add_x();
-  const int pairs = n_tiles < rec->sms / 2 ? n_tiles : rec->sms / 2;
-  a.order = plan_schedule(tiles[first], cost[first], tiles[1 - first], cost[1 - first], pairs);
+  if (!x_first && want_x) add_x();
+  a.order = t.order;
   if (!ok) return NSP_ERR_CUDA;
   a.status = rec->word;
   count_launches(1);
   const int blocks = act_args.total / 256 + 1 < 148u * 8 ? static_cast<int>(act_args.total / 256 + 1) : 148 * 8;
   if (launch_chained_if(true, act == NSP_ACT_SILU ? glu_act_kernel<kSilu> : glu_act_kernel<kGelu>, blocks, 256, 0, st, act_args) != cudaSuccess)
     return NSP_ERR_CUDA;
-  return launch_gemm<-1>(maps, a, pairs, st) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
+  return launch_gemm<-1>(maps, a, t.tall, t.pairs, st) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }
 
 extern "C" int nsp_glu_status(int32_t out[4]) {
