@@ -7,6 +7,7 @@ raises, and on a machine without a B200 the compute calls return ``NSP_ERR_CUDA`
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 
 import numpy as np
@@ -141,12 +142,12 @@ def lib() -> ctypes.CDLL:
                                            ctypes.POINTER(ctypes.c_float)]
         L.nsp_rope.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_float,
                                ctypes.c_int32, vp]
-        rows = ctypes.POINTER(Rows)
+        rows = vp  # packed Rows
         L.nsp_norm_fwd.argtypes = [rows, vp, vp, rows, vp, vp, ctypes.c_int64] + [ctypes.c_int32] * 5 + [ctypes.c_float, vp]
         L.nsp_norm_bwd_ws_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
         L.nsp_norm_bwd.argtypes = [rows, rows, vp, vp, vp, rows, vp, vp, ctypes.c_int64] + [ctypes.c_int32] * 5 + [
             vp, ctypes.c_size_t, vp]
-        matrix = ctypes.POINTER(Matrix)
+        matrix = vp  # a packed Matrix
         L.nsp_glu_fwd.argtypes = [matrix] * 6 + [ctypes.c_int64] + [ctypes.c_int32] * 3 + [vp]
         L.nsp_glu_bwd_ws_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
         L.nsp_glu_bwd.argtypes = [matrix] * 9 + [ctypes.c_int64] + [ctypes.c_int32] * 3 + [vp, ctypes.c_size_t, vp]
@@ -619,31 +620,54 @@ def nsp_attn_bwd_static(plan: Plan, q, k, v, o, d_o, lse, dq, dk, dv, softmax_sc
 
 
 # ---- token-wise operators around the attention
+# The small calls of these last about as long as the checks around them: structures are packed at once (struct) instead of field by
+# field, and every attribute of a tensor is asked for once.
+_ROPE_TENSOR, _ROWS, _MATRIX = (struct.Struct(f) for f in ("=QQQqqqqqii", "=Qqq", "=Qq"))
+
+
 def _refuse(what, why, code=NSP_ERR_INVALID_ARG):
     raise NspError(code, f"{what}: {why}")
 
 
-def _on_device(what, named, here):
-    """Refuse tensors that are not on the current device. named: (name, tensor) pairs; None is left out."""
+def _on_device(what, names, tensors):
+    """The current device; refuses tensors that are not on it (None is left out)."""
     import torch
 
-    for name, t in named:
+    here = None
+    for t in tensors:
         if t is None:
             continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        at = t.get_device() if isinstance(t, torch.Tensor) else -1
+        if at < 0:
+            name = names[[x is t for x in tensors].index(True) % len(names)]
             _refuse(what, f"{name} must be a CUDA tensor")
-        if t.get_device() != here:
+        if here is None:
+            here = torch.cuda.current_device()
+        if at != here:
+            name = names[[x is t for x in tensors].index(True) % len(names)]
             _refuse(what, f"{name} is on {t.device}, not on the current device")
+    return here
 
 
-def _dtype_of(what, name, t):
+def _stream_on(here, stream):
+    """As _stream_ptr, with the current device known."""
+    if stream is None and here is not None:
+        import torch
+
+        direct = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if direct:
+            return direct(here)
+    return _stream_ptr(stream)
+
+
+def _dtype_of(what, name, dtype):
     import torch
 
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return NSP_BF16
-    if t.dtype == torch.float32:
+    if dtype == torch.float32:
         return NSP_F32
-    _refuse(what, f"{name} has dtype {t.dtype}")
+    _refuse(what, f"{name} has dtype {dtype}")
 
 
 def nsp_rope_frequencies(rot_dim, base=10000.0, kind=NSP_ROPE_PLAIN, scale=1.0, trained_tokens=0.0, fast_turns=32.0,
@@ -675,55 +699,58 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
     freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
     if freq.ndim != 1 or len(freq) == 0:
         _refuse(what, "inv_freq holds one frequency per rotated pair")
+    if len(xs) > NSP_ROPE_MAX_TENSORS:
+        _refuse(what, f"more than {NSP_ROPE_MAX_TENSORS} tensors", NSP_ERR_UNSUPPORTED)
     if not xs:
         return
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    array = (RopeTensor * len(xs))()
-    head_dim = xs[0].shape[-1] if isinstance(xs[0], torch.Tensor) and xs[0].dim() == 3 else 0
-    for a, x, y, pos in zip(array, xs, ys, positions):
-        _on_device(what, (("x", x), ("y", y), ("positions", pos)), here)
-        if x.dim() != 3 or x.shape[2] != head_dim or y.shape != x.shape or y.dtype != x.dtype:
+    here = _on_device(what, ("x", "y", "positions"), [t for group in zip(xs, ys, positions) for t in group])
+    packed, head_dim = [], xs[0].shape[-1]
+    for x, y, pos in zip(xs, ys, positions):
+        shape, dtype, sx, sy = x.shape, x.dtype, x.stride(), y.stride()
+        if len(shape) != 3 or shape[2] != head_dim or y.shape != shape or y.dtype != dtype:
             _refuse(what, "x and y are [tokens, heads, head_dim] of one shape and type, with one head_dim in all")
-        if head_dim > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+        if head_dim > 1 and (sx[2] != 1 or sy[2] != 1):
             _refuse(what, "the elements of a head must be contiguous")
-        if pos is not None and (pos.dtype != torch.int64 or pos.dim() != 1 or not pos.is_contiguous() or pos.numel() != x.shape[0]):
+        tokens, heads = shape[0], shape[1]
+        if pos is not None and (pos.dtype != torch.int64 or pos.shape != (tokens,) or not pos.is_contiguous()):
             _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
-        a.dtype = _dtype_of(what, "x", x)
-        if x.numel() == 0:
-            a.heads = max(x.shape[1], 1)  # tokens = 0: nothing to do
+        if tokens * heads * head_dim == 0:
             continue
-        a.x, a.y, a.positions = x.data_ptr(), y.data_ptr(), None if pos is None else pos.data_ptr()
-        a.tokens, a.heads = x.shape[0], x.shape[1]
-        a.x_token_stride, a.x_head_stride = x.stride(0), x.stride(1)
-        a.y_token_stride, a.y_head_stride = y.stride(0), y.stride(1)
-    rc = lib().nsp_rope(array, len(xs), head_dim, 2 * len(freq), int(layout), _ptr(freq), float(magnitude), int(bool(inverse)),
-                        _stream_ptr(stream))
+        packed.append(_ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), 0 if pos is None else pos.data_ptr(), tokens, sx[0], sx[1], sy[0],
+                                        sy[1], heads, _dtype_of(what, "x", dtype)))
+    rc = lib().nsp_rope(b"".join(packed), len(packed), head_dim, 2 * len(freq), int(layout), freq.tobytes(), float(magnitude),
+                        1 if inverse else 0, _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
 
 
-def _rows(what, name, t, like=None):
-    """(Rows, outer, inner, dim) of a tensor [rows, dim] or [outer, inner, dim] with contiguous last axis."""
-    if t.dim() not in (2, 3) or (like is not None and (t.shape != like.shape or t.dtype != like.dtype)):
-        _refuse(what, f"{name} must be [rows, dim] or [outer, inner, dim]" + (", of x's shape and type" if like is not None else ""))
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _rows(what, name, t, shape, dtype):
+    """A packed nsp_rows_t of a tensor [rows, dim] or [outer, inner, dim] of that shape and type, with contiguous last axis."""
+    if t.shape != shape or t.dtype != dtype:
+        _refuse(what, f"{name} must have x's shape and type")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         _refuse(what, f"the last axis of {name} must be contiguous")
-    three = t.dim() == 3
-    return (Rows(t.data_ptr() or None, t.stride(0), t.stride(1) if three else 0), t.shape[0], t.shape[1] if three else 1, t.shape[-1])
+    return _ROWS.pack(t.data_ptr(), strides[0], strides[1] if len(strides) == 3 else 0)
 
 
-def _norm_vectors(what, named, dim, dtypes):
-    for name, t in named:
-        if t is not None and (t.numel() != dim or not t.is_contiguous() or t.dtype not in dtypes):
-            _refuse(what, f"{name} must be contiguous, with {dim} elements of {dtypes}")
+def _norm_shape(what, x):
+    """(outer, inner, dim, dtype code) of x."""
+    shape = x.shape
+    if len(shape) == 2:
+        return shape[0], 1, shape[1], _dtype_of(what, "x", x.dtype)
+    if len(shape) == 3:
+        return shape[0], shape[1], shape[2], _dtype_of(what, "x", x.dtype)
+    _refuse(what, "x must be [rows, dim] or [outer, inner, dim]")
 
 
-def _norm_stats(what, named, rows):
-    import torch
-
-    for name, t in named:
-        if t is not None and (t.numel() != rows or not t.is_contiguous() or t.dtype != torch.float32):
-            _refuse(what, f"{name} must be a contiguous float32 tensor with one entry per row ({rows})")
+def _norm_vector(what, name, t, n, dtypes):
+    """Address of a contiguous tensor of n elements of these types; None: a null pointer."""
+    if t is None:
+        return None
+    if t.numel() != n or t.dtype not in dtypes or not t.is_contiguous():
+        _refuse(what, f"{name} must be contiguous, with {n} elements of {dtypes}")
+    return t.data_ptr()
 
 
 def nsp_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NSP_NORM_LAYER, stream=None):
@@ -731,21 +758,20 @@ def nsp_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NSP_NORM_LAYER, 
     (bf16 or fp32, None = 1 and 0); mean, rstd: fp32, one entry per row, for the backward pass (None: not wanted)."""
     import torch
 
-    what = "nsp_norm_fwd"
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    _on_device(what, (("x", x), ("y", y), ("weight", weight), ("bias", bias), ("mean", mean), ("rstd", rstd)), here)
-    rx, outer, inner, dim = _rows(what, "x", x)
-    ry = _rows(what, "y", y, x)[0]
-    _norm_vectors(what, (("weight", weight), ("bias", bias)), dim, (torch.bfloat16, torch.float32))
+    what, both, f32 = "nsp_norm_fwd", (torch.float32, torch.bfloat16), (torch.float32,)
+    here = _on_device(what, ("x", "y", "weight", "bias", "mean", "rstd"), (x, y, weight, bias, mean, rstd))
+    outer, inner, dim, dtype = _norm_shape(what, x)
+    rows = outer * inner
+    rx, ry = _rows(what, "x", x, x.shape, x.dtype), _rows(what, "y", y, x.shape, x.dtype)
+    w, b = _norm_vector(what, "weight", weight, dim, both), _norm_vector(what, "bias", bias, dim, both)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         _refuse(what, "weight and bias have one type")
-    _norm_stats(what, (("mean", mean), ("rstd", rstd)), outer * inner)
-    dtype = _dtype_of(what, "x", x)
-    if outer * inner == 0 or dim == 0:
+    m, r = _norm_vector(what, "mean", mean, rows, f32), _norm_vector(what, "rstd", rstd, rows, f32)
+    if rows == 0 or dim == 0:
         return
     one = weight if weight is not None else bias
-    rc = lib().nsp_norm_fwd(ctypes.byref(rx), _ptr(weight), _ptr(bias), ctypes.byref(ry), _ptr(mean), _ptr(rstd), outer, inner, dim, dtype,
-                            NSP_F32 if one is None else _dtype_of(what, "weight", one), int(kind), float(eps), _stream_ptr(stream))
+    w_dtype = NSP_BF16 if one is not None and one.dtype == torch.bfloat16 else NSP_F32
+    rc = lib().nsp_norm_fwd(rx, w, b, ry, m, r, outer, inner, dim, dtype, w_dtype, int(kind), float(eps), _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
 
@@ -764,60 +790,58 @@ def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NOR
     is wanted)."""
     import torch
 
-    what = "nsp_norm_bwd"
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    _on_device(what, (("x", x), ("dy", dy), ("dx", dx), ("weight", weight), ("mean", mean), ("rstd", rstd), ("dweight", dweight),
-                      ("dbias", dbias), ("ws", ws)), here)
-    rx, outer, inner, dim = _rows(what, "x", x)
-    rdy, rdx = _rows(what, "dy", dy, x)[0], _rows(what, "dx", dx, x)[0]
-    _norm_vectors(what, (("weight", weight),), dim, (torch.bfloat16, torch.float32))
-    _norm_vectors(what, (("dweight", dweight), ("dbias", dbias)), dim, (torch.float32,))
-    _norm_stats(what, (("mean", mean), ("rstd", rstd)), outer * inner)
+    what, both, f32 = "nsp_norm_bwd", (torch.float32, torch.bfloat16), (torch.float32,)
+    here = _on_device(what, ("x", "dy", "dx", "weight", "mean", "rstd", "dweight", "dbias", "ws"),
+                      (x, dy, dx, weight, mean, rstd, dweight, dbias, ws))
+    outer, inner, dim, dtype = _norm_shape(what, x)
+    rows = outer * inner
+    rx, rdy, rdx = (_rows(what, name, t, x.shape, x.dtype) for name, t in (("x", x), ("dy", dy), ("dx", dx)))
+    w = _norm_vector(what, "weight", weight, dim, both)
+    dw, db = _norm_vector(what, "dweight", dweight, dim, f32), _norm_vector(what, "dbias", dbias, dim, f32)
     if rstd is None or (mean is None and kind == NSP_NORM_LAYER):
         _refuse(what, "the forward pass's statistics are needed")
+    m, r = _norm_vector(what, "mean", mean, rows, f32), _norm_vector(what, "rstd", rstd, rows, f32)
     _check_ws(what, ws)
-    dtype = _dtype_of(what, "x", x)
     if dim == 0:
         return
-    rc = lib().nsp_norm_bwd(ctypes.byref(rx), ctypes.byref(rdy), _ptr(weight), _ptr(mean), _ptr(rstd), ctypes.byref(rdx), _ptr(dweight),
-                            _ptr(dbias), outer, inner if outer * inner else 1, dim, dtype,
-                            NSP_F32 if weight is None else _dtype_of(what, "weight", weight), int(kind), _ptr(ws),
-                            0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream))
+    w_dtype = NSP_BF16 if weight is not None and weight.dtype == torch.bfloat16 else NSP_F32
+    rc = lib().nsp_norm_bwd(rx, rdy, w, m, r, rdx, dw, db, outer if rows else 0, inner if rows else 1, dim, dtype, w_dtype, int(kind),
+                            None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
+                            _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
 
 
 def _matrix(what, name, t, rows, cols):
-    """Matrix of a bf16 tensor [rows, cols] with contiguous rows (None: a null pointer)."""
+    """A packed nsp_matrix_t of a bf16 tensor [rows, cols] with contiguous rows (None: a null pointer)."""
     import torch
 
     if t is None:
         return None
     if t.dtype != torch.bfloat16:
         _refuse(what, f"{name} has dtype {t.dtype}")
-    if tuple(t.shape) != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+    strides = t.stride()
+    if t.shape != (rows, cols) or (cols > 1 and strides[1] != 1):
         _refuse(what, f"{name} must be [{rows}, {cols}] with contiguous rows")
-    return ctypes.byref(Matrix(t.data_ptr() or None, t.stride(0)))
+    return _MATRIX.pack(t.data_ptr(), strides[0])
 
 
 def _glu_sizes(what, x, w_gate):
-    if x.dim() != 2 or w_gate.dim() != 2:
+    sx, sw = x.shape, w_gate.shape
+    if len(sx) != 2 or len(sw) != 2:
         _refuse(what, "x is [rows, d_model], w_gate and w_up are [d_ff, d_model]")
-    return x.shape[0], x.shape[1], w_gate.shape[0]
+    return sx[0], sx[1], sw[0]
 
 
 def nsp_glu_fwd(x, w_gate, w_up, h, g=None, u=None, act=NSP_ACT_SILU, stream=None):
     """h = act(x w_gate^T) * (x w_up^T), bf16 tensors x [rows, d_model], w_gate and w_up [d_ff, d_model], h [rows, d_ff]; g and u
     (as h): the two projections, for the backward pass."""
-    import torch
-
     what = "nsp_glu_fwd"
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    _on_device(what, (("x", x), ("w_gate", w_gate), ("w_up", w_up), ("h", h), ("g", g), ("u", u)), here)
+    here = _on_device(what, ("x", "w_gate", "w_up", "h", "g", "u"), (x, w_gate, w_up, h, g, u))
     rows, d, f = _glu_sizes(what, x, w_gate)
     rc = lib().nsp_glu_fwd(_matrix(what, "x", x, rows, d), _matrix(what, "w_gate", w_gate, f, d), _matrix(what, "w_up", w_up, f, d),
                            _matrix(what, "h", h, rows, f), _matrix(what, "g", g, rows, f), _matrix(what, "u", u, rows, f), rows, d, f,
-                           int(act), _stream_ptr(stream))
+                           int(act), _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
 
@@ -833,18 +857,16 @@ def nsp_glu_bwd_ws_bytes(rows, d_model, d_ff) -> int:
 def nsp_glu_bwd(dh, x, w_gate, w_up, g, u, dx, dw_gate, dw_up, ws, act=NSP_ACT_SILU, stream=None):
     """Backward pass of nsp_glu_fwd from dh and the g, u it saved: dx (None: not wanted), dw_gate and dw_up (both None: not
     wanted), overwritten. ws: a CUDA tensor of at least nsp_glu_bwd_ws_bytes(rows, d_model, d_ff) bytes."""
-    import torch
-
     what = "nsp_glu_bwd"
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    _on_device(what, (("dh", dh), ("x", x), ("w_gate", w_gate), ("w_up", w_up), ("g", g), ("u", u), ("dx", dx), ("dw_gate", dw_gate),
-                      ("dw_up", dw_up), ("ws", ws)), here)
+    here = _on_device(what, ("dh", "x", "w_gate", "w_up", "g", "u", "dx", "dw_gate", "dw_up", "ws"),
+                      (dh, x, w_gate, w_up, g, u, dx, dw_gate, dw_up, ws))
     rows, d, f = _glu_sizes(what, x, w_gate)
     _check_ws(what, ws)
     rc = lib().nsp_glu_bwd(_matrix(what, "dh", dh, rows, f), _matrix(what, "x", x, rows, d), _matrix(what, "w_gate", w_gate, f, d),
                            _matrix(what, "w_up", w_up, f, d), _matrix(what, "g", g, rows, f), _matrix(what, "u", u, rows, f),
                            _matrix(what, "dx", dx, rows, d), _matrix(what, "dw_gate", dw_gate, f, d), _matrix(what, "dw_up", dw_up, f, d),
-                           rows, d, f, int(act), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream))
+                           rows, d, f, int(act), None if ws is None else ws.data_ptr(),
+                           0 if ws is None else ws.numel() * ws.element_size(), _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
 

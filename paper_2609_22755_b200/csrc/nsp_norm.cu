@@ -7,15 +7,16 @@
 // sums would lose the variance of rows that lie far from zero).
 //
 // Teams. A row belongs to a team of threads: some lanes of a warp, a warp or several warps; thread i of it has the vectors i,
-// i + team, ... of 8 elements. In the forward pass a lane has up to 16 vectors, so that a row of 4,096 is one warp's: no barrier,
-// and loads of a whole row under way in every warp. In the backward pass a thread keeps the parameters' gradients of its columns in
-// fp32 registers over all rows it meets, which bounds its columns to 16 or 32; long rows are a block's, come through shared memory
-// some rows ahead by asynchronous copies (each thread copies and reads its own vectors: no barrier either), and the sums of
-// one or two rows are exchanged at one barrier. The blocks' gradients go to the workspace and a second kernel adds them in their
-// order: the same bits in every run.
+// i + team, ... of 8 elements. In the forward pass a team takes up to four rows together, whose loads are all under way at once
+// and which share the loads of the parameters (twice the bytes of a row in bf16, where they are fp32) and the barriers of their
+// sums. In the backward pass a thread keeps the parameters' gradients of its columns in fp32 registers over all rows it meets,
+// which bounds its columns to 16 or 32; long rows come through shared memory some rows ahead by asynchronous copies (each thread
+// copies and reads its own vectors: no barrier), and a row's sums are exchanged at one barrier. The blocks'
+// gradients go to the workspace and a second kernel adds them in their order: the same bits in every run.
 // Rows whose addresses do not allow vectors go element by element, through kernels of their own (norm_*_element_kernel).
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include "nsp_internal.cuh"
@@ -44,7 +45,7 @@ struct NormArgs {
   float* rstd;
   float* part;  // [2][blocks][dim]: sums of a block for dw, db
   int64_t rows;
-  int32_t inner, dim, w_f32, want_grads, stages;
+  int32_t inner, dim, w_f32, want_grads, stages, team;  // long rows: stages of the copies, threads of a row
   float eps, inv_dim;
 };
 
@@ -162,6 +163,32 @@ struct RowWalk {
     if (i >= inner) i -= inner, ++o;
   }
   __device__ __forceinline__ char* at(const NormRows& t) const { return t.p + o * t.outer + i * t.inner; }
+};
+
+// The same rows of several tensors as addresses: an addition a step, and one more where a step passes the end of the inner axis.
+template <int N>
+struct PointerWalk {
+  char* p[N];
+  int64_t step[N], wrap[N], r, r_step;
+  int32_t i, i_step, inner;
+  __device__ __forceinline__ PointerWalk(const NormRows (&t)[N], int64_t first, int64_t step_, int32_t inner_, int64_t more)
+      : r(first), r_step(step_), inner(inner_) {
+    const int64_t o = r / inner, o_step = step_ / inner;
+    i = static_cast<int32_t>(r - o * inner), i_step = static_cast<int32_t>(step_ - o_step * inner);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      p[k] = t[k].p + o * t[k].outer + i * t[k].inner + more;
+      step[k] = o_step * t[k].outer + i_step * t[k].inner;
+      wrap[k] = t[k].outer - inner * t[k].inner;
+    }
+  }
+  __device__ __forceinline__ void next() {
+    r += r_step, i += i_step;
+    const bool past = i >= inner;
+    if (past) i -= inner;
+#pragma unroll
+    for (int k = 0; k < N; ++k) p[k] += step[k] + (past ? wrap[k] : 0);
+  }
 };
 
 template <typename T, int V, int NV, int kTeam, bool kLayer>
@@ -380,11 +407,14 @@ __device__ __forceinline__ void row_of(uint32_t r, int inner, int64_t& o, int& i
 }
 
 // kLanes lanes (a warp: kWarps of them) a row, kVecs vectors a lane, kRows rows a team
+constexpr int fwd_threads(int warps) { return warps > 4 ? 32 * warps : 128; }
+// Blocks an SM the registers are cut to: five where four vectors a lane are under way (2,048: 50 -> 46 us for 32,768 rows), else the
+// compiler's choice (512: 50 us, cut 54).
+constexpr int fwd_blocks(int vecs, int warps) { return vecs != 4 ? 1 : warps <= 4 ? 5 : warps == 8 ? 2 : 1; }
 template <typename T, int kLanes, int kVecs, int kWarps, int kRows, bool kLayer>
-__global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kernel(const NormArgs a) {
-  constexpr int kTeam = kLanes * kWarps, kBlock = kWarps > 4 ? 32 * kWarps : 128, kTeams = kBlock / kTeam;
-  static_assert(kWarps == 1 || kRows == 1, "rows of several warps one at a time");
-  __shared__ float part[2][kWarps > 1 ? kTeams : 1][kWarps];
+__global__ void __launch_bounds__(fwd_threads(kWarps), fwd_blocks(kVecs, kWarps)) norm_fwd_kernel(const NormArgs a) {
+  constexpr int kTeam = kLanes * kWarps, kTeams = fwd_threads(kWarps) / kTeam;
+  __shared__ __align__(16) float part[2][kWarps > 1 ? kTeams : 1][kRows][kWarps];
   const int lane = static_cast<int>(threadIdx.x) % kTeam, team = static_cast<int>(threadIdx.x) / kTeam;
   const int n_vec = a.dim / 8;
   grid_wait_predecessor();
@@ -392,32 +422,39 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
   const int64_t first = (static_cast<int64_t>(blockIdx.x) * kTeams + team) * kRows;
   Vec<T, 8> x[kRows][kVecs];
   char* out[kRows];
-#pragma unroll
-  for (int q = 0; q < kRows; ++q) {
+  {
     int64_t o;
     int i;
-    row_of(static_cast<uint32_t>(first + q), a.inner, o, i);
-    const char* row = a.x.p + o * a.x.outer + i * a.x.inner;
-    out[q] = a.y.p + o * a.y.outer + i * a.y.inner;
+    row_of(static_cast<uint32_t>(first), a.inner, o, i);
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      x[q][j].zero();
-      if (first + q < a.rows && lane + j * kTeam < n_vec) x[q][j].load(row, lane + j * kTeam);
+    for (int q = 0; q < kRows; ++q) {
+      const char* row = a.x.p + o * a.x.outer + i * a.x.inner;
+      out[q] = a.y.p + o * a.y.outer + i * a.y.inner;
+      if (++i == a.inner) i = 0, ++o;
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+        x[q][j].zero();
+        if (first + q < a.rows && lane + j * kTeam < n_vec) x[q][j].load(row, lane + j * kTeam);
+      }
     }
   }
-  // the same sum in all threads of a team
+  // the same sums in all threads of a team
   auto team_sum = [&](float (&v)[kRows], [[maybe_unused]] int turn) {
+    const float one = lanes_sum<kRows, kLanes>(v, lane % kLanes);
+    if constexpr (kWarps == 1) {
 #pragma unroll
-    for (int o = kLanes / 2; o > 0; o /= 2) {
+      for (int q = 0; q < kRows; ++q) v[q] = __shfl_sync(0xffffffffu, one, sum_at<kRows, kLanes>(q), kLanes);
+    } else {
 #pragma unroll
-      for (int q = 0; q < kRows; ++q) v[q] += __shfl_xor_sync(0xffffffffu, v[q], o);
-    }
-    if constexpr (kWarps > 1) {
-      if (lane % 32 == 0) part[turn][team][lane / 32] = v[0];
+      for (int q = 0; q < kRows; ++q)
+        if (lane % 32 == sum_at<kRows, 32>(q)) part[turn][team][q][lane / 32] = one;
       __syncthreads();
-      v[0] = part[turn][team][0];
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) v[0] += part[turn][team][w];
+      for (int q = 0; q < kRows; ++q) {
+        v[q] = part[turn][team][q][0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) v[q] += part[turn][team][q][w];
+      }
     }
   };
   float mu[kRows], rstd[kRows];
@@ -426,13 +463,13 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
   if (kLayer) {
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int j = 0; j < kVecs; ++j) {
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) add2(s[k % 4], s[k % 4 + 1], s[k % 4], s[k % 4 + 1], x[q][j].get(k), x[q][j].get(k + 1));
+        for (int k = 0; k < 8; k += 2) add2(s0, s1, s0, s1, x[q][j].get(k), x[q][j].get(k + 1));
       }
-      mu[q] = (s[0] + s[2]) + (s[1] + s[3]);
+      mu[q] = s0 + s1;
     }
     team_sum(mu, 0);
 #pragma unroll
@@ -440,7 +477,7 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
   }
 #pragma unroll
   for (int q = 0; q < kRows; ++q) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
       if (!kLayer || lane + j * kTeam < n_vec) {
@@ -448,11 +485,11 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
         for (int k = 0; k < 8; k += 2) {
           float d0 = x[q][j].get(k), d1 = x[q][j].get(k + 1);
           if (kLayer) add2(d0, d1, d0, d1, -mu[q], -mu[q]);
-          fma2(s[k % 4], s[k % 4 + 1], d0, d1, d0, d1, s[k % 4], s[k % 4 + 1]);
+          fma2(s0, s1, d0, d1, d0, d1, s0, s1);
         }
       }
     }
-    rstd[q] = (s[0] + s[2]) + (s[1] + s[3]);
+    rstd[q] = s0 + s1;
   }
   team_sum(rstd, 1);
 #pragma unroll
@@ -462,6 +499,7 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
       if (a.rstd) a.rstd[first + q] = rstd[q];
       if (kLayer && a.mean) a.mean[first + q] = mu[q];
     }
+    mu[q] *= -rstd[q];  // (x - mu) r = x r - mu r, one rounding of mu r like the one of mu
   }
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
@@ -475,9 +513,11 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
         float y[8];
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
-          float d0 = x[q][j].get(k), d1 = x[q][j].get(k + 1);
-          if (kLayer) add2(d0, d1, d0, d1, -mu[q], -mu[q]);
-          mul2(d0, d1, d0, d1, rstd[q], rstd[q]);
+          float d0, d1;
+          if (kLayer)
+            fma2(d0, d1, x[q][j].get(k), x[q][j].get(k + 1), rstd[q], rstd[q], mu[q], mu[q]);
+          else
+            mul2(d0, d1, x[q][j].get(k), x[q][j].get(k + 1), rstd[q], rstd[q]);
           fma2(y[k], y[k + 1], d0, d1, w[k], w[k + 1], b[k], b[k + 1]);
         }
         if (first + q < a.rows) Vec<T, 8>::store(out[q], v, y);
@@ -486,48 +526,81 @@ __global__ void __launch_bounds__(kWarps > 4 ? 32 * kWarps : 128) norm_fwd_kerne
   }
 }
 
-// What a thread does with a vector of a row: the sums of t h and t, the parameters' gradients, and dx.
+// What a thread does with a vector of a row: the sums of t h and t and the parameters' gradients, and dx. A row's constants:
+//     h = x r + shift, shift = -mu r;   dx = r t + x slope + offset, slope = -r^2 c1, offset = -r (c1 shift + c2)
+// with c1 = mean(t h), c2 = mean(t): the products of h are taken apart so that a pair of elements takes three instructions.
 enum : int { kRms = 0, kRmsBias = 1, kLayerBias = 2 };  // whether mean(t) is subtracted and db is summed up
+// Pairs of fp32 in one 64-bit register, as the packed instructions take them.
+struct F2 {
+  uint64_t v;
+  __device__ __forceinline__ static F2 of(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+  }
+  __device__ __forceinline__ float lo() const { return __uint_as_float(static_cast<uint32_t>(v)); }
+  __device__ __forceinline__ float hi() const { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+  __device__ __forceinline__ float sum() const { return lo() + hi(); }
+};
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 template <typename T, int kKind>
 struct BwdVec {
-  __device__ __forceinline__ static void sums(const Vec<T, 8>& x, const Vec<T, 8>& dy, const float (&w)[8], float r, float shift, float (&s)[2],
-                                              float (&c)[2], float (&dw)[8], float (&db)[8]) {
+  struct Params {  // of the 8 columns of a vector
+    F2 v[4];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      float h0, h1, t0, t1;
-      const float g0 = dy.get(k), g1 = dy.get(k + 1);
-      hat(x, k, r, shift, h0, h1);
-      mul2(t0, t1, g0, g1, w[k], w[k + 1]);
-      fma2(s[0], s[1], t0, t1, h0, h1, s[0], s[1]);
-      if (kKind == kLayerBias) add2(c[0], c[1], c[0], c[1], t0, t1);
-      fma2(dw[k], dw[k + 1], g0, g1, h0, h1, dw[k], dw[k + 1]);
-      if (kKind != kRms) add2(db[k], db[k + 1], db[k], db[k + 1], g0, g1);
+      for (F2& x : v) x.v = 0;
+    }
+    __device__ __forceinline__ void load(const NormArgs& a, int c) {
+      float w[8];
+      load_params<8>(a.w, a.w_f32, c, 1.f, w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = F2::of(w[2 * k], w[2 * k + 1]);
+    }
+  };
+  __device__ __forceinline__ static F2 pair(const Vec<T, 8>& x, int k) { return F2::of(x.get(2 * k), x.get(2 * k + 1)); }
+  __device__ __forceinline__ static void sums(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 shift, F2& s, F2& c, Params& dw,
+                                              Params& db) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const F2 g = pair(dy, k), u = pair(x, k);
+      const F2 gh = mul(kKind == kLayerBias ? fma(u, r, shift) : mul(u, r), g);
+      s = fma(w.v[k], gh, s);
+      dw.v[k] = add(dw.v[k], gh);
+      if (kKind == kLayerBias) c = fma(w.v[k], g, c);
+      if (kKind != kRms) db.v[k] = add(db.v[k], g);
     }
   }
-  // h = (x - mu) r; `shift` is -mu
-  __device__ __forceinline__ static void hat(const Vec<T, 8>& x, int k, float r, float shift, float& h0, float& h1) {
-    h0 = x.get(k), h1 = x.get(k + 1);
-    if (kKind == kLayerBias) add2(h0, h1, h0, h1, shift, shift);
-    mul2(h0, h1, h0, h1, r, r);
-  }
-  // r (t - c2 - h c1)
-  __device__ __forceinline__ static void grad(const Vec<T, 8>& x, const Vec<T, 8>& dy, const float (&w)[8], float r, float shift, float c1,
-                                              float c2, char* out, int v) {
+  __device__ __forceinline__ static void grad(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 slope, F2 offset, char* out, int v,
+                                              bool here = true) {
     float o[8];
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      float h0, h1, t0, t1;
-      hat(x, k, r, shift, h0, h1);
-      if (kKind == kLayerBias)
-        fma2(t0, t1, dy.get(k), dy.get(k + 1), w[k], w[k + 1], -c2, -c2);
-      else
-        mul2(t0, t1, dy.get(k), dy.get(k + 1), w[k], w[k + 1]);
-      fma2(t0, t1, h0, h1, -c1, -c1, t0, t1);
-      mul2(o[k], o[k + 1], t0, t1, r, r);
+    for (int k = 0; k < 4; ++k) {
+      const F2 u = pair(x, k);
+      const F2 d = fma(mul(pair(dy, k), w.v[k]), r, kKind == kLayerBias ? fma(u, slope, offset) : mul(u, slope));
+      o[2 * k] = d.lo(), o[2 * k + 1] = d.hi();
     }
-    Vec<T, 8>::store(out, v, o);
+    if (here) Vec<T, 8>::store(out, v, o);
   }
+  __device__ __forceinline__ static float slope(float r, float c1) { return -r * r * c1; }
+  __device__ __forceinline__ static float offset(float r, float shift, float c1, float c2) { return -r * fmaf(c1, shift, c2); }
 };
+__device__ __forceinline__ F2 both(float x) { return F2::of(x, x); }
 
 // Short rows: kLanes lanes of a warp a row, kRows rows at a time
 template <typename T, int kLanes, int kVecs, int kRows, int kKind>
@@ -535,17 +608,15 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
   constexpr int kTeams = 256 / kLanes, kSums = kRows * (kKind == kLayerBias ? 2 : 1);
   const int lane = static_cast<int>(threadIdx.x) % kLanes, team = static_cast<int>(threadIdx.x) / kLanes;
   const int n_vec = a.dim / 8;
-  float dw[kVecs][8], db[kVecs][8], w[kVecs][8];
+  using B = BwdVec<T, kKind>;
+  typename B::Params dw[kVecs], db[kVecs], w[kVecs];
 #pragma unroll
-  for (int j = 0; j < kVecs; ++j) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dw[j][k] = 0.f, db[j][k] = 0.f, w[j][k] = 0.f;
-  }
+  for (int j = 0; j < kVecs; ++j) dw[j].zero(), db[j].zero(), w[j].zero();
   grid_wait_predecessor();
   grid_launch_dependents();
 #pragma unroll
   for (int j = 0; j < kVecs; ++j)
-    if (lane + j * kLanes < n_vec) load_params<8>(a.w, a.w_f32, (lane + j * kLanes) * 8, 1.f, w[j]);
+    if (lane + j * kLanes < n_vec) w[j].load(a, (lane + j * kLanes) * 8);
   const int64_t step = static_cast<int64_t>(gridDim.x) * kTeams * kRows;
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * kTeams * kRows; base < a.rows; base += step) {
     Vec<T, 8> x[kRows][kVecs], dy[kRows][kVecs];
@@ -566,28 +637,29 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
         if (here && lane + j * kLanes < n_vec) x[q][j].load(px, lane + j * kLanes), dy[q][j].load(pg, lane + j * kLanes);
       }
       r[q] = here ? a.rstd[row] : 0.f;
-      shift[q] = kKind == kLayerBias && here ? -a.mean[row] : 0.f;
+      shift[q] = kKind == kLayerBias && here ? -a.mean[row] * r[q] : 0.f;
     }
     float sum[kSums];
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
-      float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
+      F2 s{0}, c{0};
 #pragma unroll
       for (int j = 0; j < kVecs; ++j)
-        if (lane + j * kLanes < n_vec) BwdVec<T, kKind>::sums(x[q][j], dy[q][j], w[j], r[q], shift[q], s, c, dw[j], db[j]);
-      sum[q] = s[0] + s[1];
-      if (kKind == kLayerBias) sum[kRows + q] = c[0] + c[1];
+        if (lane + j * kLanes < n_vec) B::sums(x[q][j], dy[q][j], w[j], both(r[q]), both(shift[q]), s, c, dw[j], db[j]);
+      sum[q] = s.sum();
+      if (kKind == kLayerBias) sum[kRows + q] = c.sum();
     }
     const float mine = lanes_sum<kSums, kLanes>(sum, lane) * a.inv_dim;
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       const float c1 = __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(q), kLanes);
       const float c2 = kKind == kLayerBias ? __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(kRows + q), kLanes) : 0.f;
+      const float slope = B::slope(r[q], c1), offset = B::offset(r[q], shift[q], c1, c2);
       if (out[q]) {
 #pragma unroll
         for (int j = 0; j < kVecs; ++j)
           if (lane + j * kLanes < n_vec)
-            BwdVec<T, kKind>::grad(x[q][j], dy[q][j], w[j], r[q], shift[q], c1, c2, out[q], lane + j * kLanes);
+            B::grad(x[q][j], dy[q][j], w[j], both(r[q]), both(slope), both(offset), out[q], lane + j * kLanes);
       }
     }
   }
@@ -602,7 +674,10 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum[team][(lane + j * kLanes) * 8 + k] = pass ? db[j][k] : dw[j][k];
+      for (int k = 0; k < 4; ++k) {
+        const F2 v = pass ? db[j].v[k] : dw[j].v[k];
+        sum[team][(lane + j * kLanes) * 8 + 2 * k] = v.lo(), sum[team][(lane + j * kLanes) * 8 + 2 * k + 1] = v.hi();
+      }
     }
     __syncthreads();
     for (int c = threadIdx.x; c < a.dim; c += 256) {
@@ -614,136 +689,169 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
   }
 }
 
-// Long rows: a block a row, kVecs vectors a thread, kRows rows at a time, a.stages of these ahead
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// Long rows: several warps a row, kVecs vectors a thread, a.stages rows ahead. A block has one or more teams, which go on together (one
+// barrier a row). One row at a time: two at one barrier take more registers than two blocks an SM have (32,768 x 4,096: 141 us, with
+// two rows 276, and 512 threads of one vector 298).
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, uint32_t bytes) {  // 16, or none: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-template <typename T, int kVecs, int kRows, int kKind>
-__global__ void __launch_bounds__(512) norm_bwd_long_kernel(const NormArgs a) {
-  constexpr int kParts = kRows * (kKind == kLayerBias ? 2 : 1), kVecBytes = 8 * static_cast<int>(sizeof(T));
-  extern __shared__ __align__(16) char ring[];  // [stages][rows][x, dy][threads * kVecs] vectors
-  __shared__ __align__(16) float part[2][kParts][16];
-  const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31;
-  const int n_vec = a.dim / 8, stages = a.stages;
-  const uint32_t row_bytes = static_cast<uint32_t>(threads) * kVecs * kVecBytes, stage_bytes = 2 * kRows * row_bytes;
-  float dw[kVecs][8], db[kVecs][8];
+template <typename T, int kThreads, int kVecs, int kKind>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel(const NormArgs a) {
+  constexpr int kParts = kKind == kLayerBias ? 2 : 1, kVecBytes = 8 * static_cast<int>(sizeof(T));
+  constexpr uint32_t kVecRow = kThreads * kVecBytes, kRowBytes = kVecRow * kVecs, kStageBytes = 2 * kRowBytes;
+  extern __shared__ __align__(16) char ring[];  // [stages][x, dy][kVecs][threads] vectors; then the teams' gradients
+  __shared__ __align__(16) float part[2][kParts][kThreads / 32];
+  const int team_threads = a.team, teams = kThreads / team_threads;  // the threads behind the last team have no vectors
+  const int team = static_cast<int>(threadIdx.x) / team_threads, tid = static_cast<int>(threadIdx.x) - team * team_threads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team_warps = team_threads >> 5;
+  const int n_vec = team < teams ? a.dim / 8 : 0, stages = a.stages;
+  // Weights and the row stay in registers between the sums and dx; with four vectors a thread there is no room for them: the weights
+  // are loaded again, and the row is read again from its stage, which is then filled anew behind that.
+  constexpr int kHeld = kVecs > 2 ? 0 : kVecs;
+  using B = BwdVec<T, kKind>;
+  typename B::Params dw[kVecs], db[kVecs], held[kHeld ? kHeld : 1];
+  bool on[kVecs];
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dw[j][k] = 0.f, db[j][k] = 0.f;
+    on[j] = tid + j * team_threads < n_vec;
+    dw[j].zero(), db[j].zero();
   }
-  for (int i = tid; i < 2 * kParts * 16; i += threads) (&part[0][0][0])[i] = 0.f;
   grid_wait_predecessor();
   grid_launch_dependents();
-  const uint32_t mine = smem_u32(ring) + tid * kVecBytes;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
-  // The copies of the rows base .. base + kRows - 1 (one group, empty behind the last row)
-  auto fetch = [&](int64_t base, int stage) {
-    const uint32_t to = mine + stage * stage_bytes;
 #pragma unroll
-    for (int q = 0; q < kRows; ++q) {
-      if (base + q < a.rows) {
-        int64_t o;
-        int i;
-        row_of(static_cast<uint32_t>(base + q), a.inner, o, i);
-        const char *px = a.x.p + o * a.x.outer + i * a.x.inner, *pg = a.dy.p + o * a.dy.outer + i * a.dy.inner;
+  for (int j = 0; j < kHeld; ++j) {
+    held[j].zero();
+    if (on[j]) held[j].load(a, (tid + j * team_threads) * 8);
+  }
+  auto weights = [&](int j) -> typename B::Params {
+    if constexpr (kHeld > 0) {
+      return held[j];
+    } else {
+      typename B::Params w;
+      w.zero();
+      if (on[j]) w.load(a, (tid + j * team_threads) * 8);
+      return w;
+    }
+  };
+  const uint32_t mine = smem_u32(ring) + threadIdx.x * kVecBytes;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * teams;
+  const int64_t start = static_cast<int64_t>(blockIdx.x) * teams + team;
+  const int64_t thread_at = static_cast<int64_t>(tid) * kVecBytes;
+  const uint32_t team_at = static_cast<uint32_t>(team_threads) * kVecBytes;
+  const NormRows in_rows[2] = {a.x, a.dy}, out_rows[1] = {a.y};
+  PointerWalk<2> in(in_rows, start, step, a.inner, thread_at);
+  PointerWalk<1> out(out_rows, start, step, a.inner, 0);
+  // The copies of the next row of the walk, one group; zeros for vectors and rows that do not exist, which then add nothing
+  auto fetch = [&](int stage) {
+    const uint32_t to = mine + stage * kStageBytes;
+    const bool here = in.r < a.rows;
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-          const int v = tid + j * threads;
-          if (v < n_vec) {
+    for (int j = 0; j < kVecs; ++j) {
+      const uint32_t bytes = here && on[j] ? 16 : 0;
 #pragma unroll
-            for (int e = 0; e < kVecBytes; e += 16) {
-              copy_async16(to + (2 * q) * row_bytes + j * threads * kVecBytes + e, px + static_cast<int64_t>(v) * kVecBytes + e);
-              copy_async16(to + (2 * q + 1) * row_bytes + j * threads * kVecBytes + e, pg + static_cast<int64_t>(v) * kVecBytes + e);
-            }
-          }
-        }
+      for (int e = 0; e < kVecBytes; e += 16) {
+        copy_async16(to + j * kVecRow + e, in.p[0] + j * team_at + e, bytes);
+        copy_async16(to + kRowBytes + j * kVecRow + e, in.p[1] + j * team_at + e, bytes);
       }
     }
+    in.next();
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  int64_t base = static_cast<int64_t>(blockIdx.x) * kRows, ahead = base;
-  for (int i = 0; i < stages; ++i, ahead += step) fetch(ahead, i);
-  __syncthreads();
-  int turn = 0;
-  for (int stage = 0; base < a.rows; base += step, ahead += step, turn ^= 1) {
+  for (int i = 0; i < stages; ++i) fetch(i);
+  float next_r, next_mu;
+  auto statistics = [&](int64_t row) {
+    next_r = row < a.rows ? __ldg(a.rstd + row) : 0.f;
+    next_mu = kKind == kLayerBias && row < a.rows ? __ldg(a.mean + row) : 0.f;
+  };
+  statistics(start);
+  int turn = 0, stage = 0;
+  const float inv_dim = a.inv_dim;
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.rows; base += step, turn ^= 1) {
+    const float r = next_r, shift = -next_mu * r;
     if (stages >= 3)
       asm volatile("cp.async.wait_group 2;" ::: "memory");
     else if (stages == 2)
       asm volatile("cp.async.wait_group 1;" ::: "memory");
     else
       asm volatile("cp.async.wait_group 0;" ::: "memory");
-    Vec<T, 8> x[kRows][kVecs], dy[kRows][kVecs];
-    float r[kRows], shift[kRows], sum[kParts];
+    const char* const from = ring + stage * kStageBytes + threadIdx.x * kVecBytes;
+    Vec<T, 8> x[kVecs], dy[kVecs];
+    auto read = [&](int j) { x[j].load(from + j * kVecRow, 0), dy[j].load(from + kRowBytes + j * kVecRow, 0); };
+    F2 s{0}, c{0};
 #pragma unroll
-    for (int q = 0; q < kRows; ++q) {
-      const bool here = base + q < a.rows;
-      r[q] = here ? __ldg(a.rstd + base + q) : 0.f;
-      shift[q] = kKind == kLayerBias && here ? -__ldg(a.mean + base + q) : 0.f;
-      const char* from = ring + static_cast<size_t>(stage) * stage_bytes + tid * kVecBytes + 2 * q * row_bytes;
-      float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < kVecs; ++j) {
-        const int v = tid + j * threads;
-        if (here && v < n_vec) {
-          x[q][j].load(from, j * threads), dy[q][j].load(from + row_bytes, j * threads);
-          float w[8];
-          load_params<8>(a.w, a.w_f32, v * 8, 1.f, w);
-          BwdVec<T, kKind>::sums(x[q][j], dy[q][j], w, r[q], shift[q], s, c, dw[j], db[j]);
-        }
-      }
-      sum[q] = s[0] + s[1];
-      if (kKind == kLayerBias) sum[kRows + q] = c[0] + c[1];
+    for (int j = 0; j < kVecs; ++j) {
+      read(j);
+      B::sums(x[j], dy[j], weights(j), both(r), both(shift), s, c, dw[j], db[j]);
     }
-    fetch(ahead, stage);  // over what this thread has just read
+    float sum[kParts];
+    sum[0] = s.sum();
+    if constexpr (kKind == kLayerBias) sum[1] = c.sum();
+    const int now = stage;
     if (++stage == stages) stage = 0;
+    if (kHeld) fetch(now);  // over what this thread has just read
+    statistics(out.r + step);
     const float one = lanes_sum<kParts, 32>(sum, lane);
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
       if (lane == sum_at<kParts, 32>(k)) part[turn][k][warp] = one;
     __syncthreads();  // the other set is written behind the next barrier but one at the earliest
+    // The warps' sums, a value in every 8 lanes (or 16, where a team has more than 8 warps), in one order for all threads
     float total[kParts];
+    {
+      constexpr int kWide = kThreads > 256 ? 16 : 8;
+      const int w = lane % kWide, k = lane / kWide, first_warp = min(team, teams - 1) * team_warps;
+      float v = k < kParts && w < team_warps ? part[turn][k][first_warp + w] : 0.f;
 #pragma unroll
-    for (int k = 0; k < kParts; ++k) {
-      float4 f = *reinterpret_cast<const float4*>(part[turn][k]);
-      float t0 = f.x + f.z, t1 = f.y + f.w;
-      for (int i = 4; i < threads >> 5; i += 4) {
-        f = *reinterpret_cast<const float4*>(part[turn][k] + i);
-        t0 += f.x + f.z, t1 += f.y + f.w;
-      }
-      total[k] = (t0 + t1) * a.inv_dim;
+      for (int o = kWide / 2; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+      v *= inv_dim;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) total[i] = __shfl_sync(0xffffffffu, v, i * kWide);
     }
+    const float c1 = total[0], c2 = kKind == kLayerBias ? total[kParts - 1] : 0.f;
+    const float slope = B::slope(r, c1), offset = B::offset(r, shift, c1, c2);
+    const bool here = out.r < a.rows;
 #pragma unroll
-    for (int q = 0; q < kRows; ++q) {
-      if (base + q < a.rows) {
-        int64_t o;
-        int i;
-        row_of(static_cast<uint32_t>(base + q), a.inner, o, i);
-        char* out = a.y.p + o * a.y.outer + i * a.y.inner;
-#pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-          const int v = tid + j * threads;
-          if (v < n_vec) {
-            float w[8];
-            load_params<8>(a.w, a.w_f32, v * 8, 1.f, w);
-            BwdVec<T, kKind>::grad(x[q][j], dy[q][j], w, r[q], shift[q], total[q], kKind == kLayerBias ? total[kRows + q] : 0.f, out, v);
-          }
-        }
-      }
+    for (int j = 0; j < kVecs; ++j) {
+      if (!kHeld) read(j);
+      B::grad(x[j], dy[j], weights(j), both(r), both(slope), both(offset), out.p[0], tid + j * team_threads, here && on[j]);
     }
+    if (!kHeld) fetch(now);
+    out.next();
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   if (!a.want_grads) return;
   float* const part_w = a.part + static_cast<int64_t>(blockIdx.x) * a.dim;
   float* const part_b = part_w + static_cast<int64_t>(gridDim.x) * a.dim;
+  // the teams of a block, added in their order
+  float* const sums = reinterpret_cast<float*>(ring);  // [teams][vectors of a team][8]
+  const int team_floats = team_threads * kVecs * 8;
 #pragma unroll
-  for (int j = 0; j < kVecs; ++j) {
-    const int v = tid + j * threads;
-    if (v < n_vec) {
+  for (int pass = 0; pass < (kKind == kRms ? 1 : 2); ++pass) {
+    float* const to = pass ? part_b : part_w;
+    if (teams > 1) {
+      __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 8; k += 4) {
-        *reinterpret_cast<float4*>(part_w + v * 8 + k) = make_float4(dw[j][k], dw[j][k + 1], dw[j][k + 2], dw[j][k + 3]);
-        if (kKind != kRms) *reinterpret_cast<float4*>(part_b + v * 8 + k) = make_float4(db[j][k], db[j][k + 1], db[j][k + 2], db[j][k + 3]);
+      for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const F2 v = pass ? db[j].v[k] : dw[j].v[k];
+          if (on[j]) *reinterpret_cast<F2*>(sums + team * team_floats + (tid + j * team_threads) * 8 + 2 * k) = v;
+        }
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.dim; c += kThreads) {
+        float t = sums[c];
+        for (int i = 1; i < teams; ++i) t += sums[i * team_floats + c];
+        to[c] = t;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+        if (on[j]) {
+          float* const at = to + (tid + j * team_threads) * 8;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *reinterpret_cast<F2*>(at + 2 * k) = pass ? db[j].v[k] : dw[j].v[k];
+        }
       }
     }
   }
@@ -777,11 +885,11 @@ __global__ void __launch_bounds__(1024) norm_grads_kernel(const float* part, int
 constexpr int kSms = 148;
 constexpr int kMostShared = 227 * 1024;
 
-// A launch: which kernel, blocks and threads, shared memory and stages of the long rows' kernel.
+// A launch: which kernel, blocks and threads; shared memory, stages and threads of a row of the long rows' kernel.
 struct Launch {
   void (*kernel)(const NormArgs) = nullptr;
   int64_t blocks = 0;
-  int threads = 0, shared = 0, stages = 0;
+  int threads = 0, shared = 0, stages = 0, team = 0;
 };
 
 int round32(int n) { return (n + 31) / 32 * 32; }
@@ -806,30 +914,35 @@ Launch element_launch(int dim, int64_t rows, bool backward) {
   return l;
 }
 
-// Vectors a lane and warps a row in the forward pass: 128 bytes of registers a lane hold 16 vectors of bf16 or 8 of fp32.
+// Vectors of a lane, warps of a row and rows of a team in the forward pass: 64 registers hold what is under way, 16 vectors of bf16 or 8
+// of fp32. Few rows go one to a team, so that they are spread over the SMs.
 template <typename T, bool kLayer>
 Launch fwd_launch(int dim, int64_t rows) {
   const int n = dim / 8;
   Launch l;
   int per_block = 0;
-  auto use = [&](void (*k)(const NormArgs), int lanes, int warps, int rows_of_team) {
-    l.kernel = k, l.threads = warps > 4 ? 32 * warps : 128, per_block = l.threads / (lanes * warps) * rows_of_team;
+  auto use = [&](auto lanes, auto vecs, auto warps, auto together) {
+    constexpr int L = decltype(lanes)::value, V = decltype(vecs)::value, W = decltype(warps)::value, R = decltype(together)::value;
+    const int teams = fwd_threads(W) / (L * W);
+    const bool spread = R > 1 && rows < static_cast<int64_t>(kSms) * 4 * teams * R;
+    if constexpr (W > 1) l.kernel = spread ? norm_fwd_kernel<T, L, V, W, 1, kLayer> : norm_fwd_kernel<T, L, V, W, R, kLayer>;
+    else l.kernel = norm_fwd_kernel<T, L, V, W, R, kLayer>;
+    l.threads = fwd_threads(W), per_block = teams * (W > 1 && spread ? 1 : R);
   };
-  if (n <= 8) use(norm_fwd_kernel<T, 8, 1, 1, 4, kLayer>, 8, 1, 4);
-  else if (n <= 16) use(norm_fwd_kernel<T, 8, 2, 1, 2, kLayer>, 8, 1, 2);
-  else if (n <= 32) use(norm_fwd_kernel<T, 16, 2, 1, 2, kLayer>, 16, 1, 2);
-  else if (n <= 64) use(norm_fwd_kernel<T, 32, 2, 1, 2, kLayer>, 32, 1, 2);
-  else if (n <= 128) use(norm_fwd_kernel<T, 32, 4, 1, 1, kLayer>, 32, 1, 1);
-  else if (n <= 256) use(norm_fwd_kernel<T, 32, 8, 1, 1, kLayer>, 32, 1, 1);
-  else if constexpr (sizeof(T) == 2) {
-    if (n <= 512) use(norm_fwd_kernel<T, 32, 16, 1, 1, kLayer>, 32, 1, 1);
-    else if (n <= 1024) use(norm_fwd_kernel<T, 32, 16, 2, 1, kLayer>, 32, 2, 1);
-    else use(norm_fwd_kernel<T, 32, 16, 4, 1, kLayer>, 32, 4, 1);
-  } else {
-    if (n <= 512) use(norm_fwd_kernel<T, 32, 8, 2, 1, kLayer>, 32, 2, 1);
-    else if (n <= 1024) use(norm_fwd_kernel<T, 32, 8, 4, 1, kLayer>, 32, 4, 1);
-    else use(norm_fwd_kernel<T, 32, 8, 8, 1, kLayer>, 32, 8, 1);
+#define NSP_USE(L, V, W, R) use(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}, std::integral_constant<int, W>{}, std::integral_constant<int, R>{})
+  if (n <= 8) NSP_USE(8, 1, 1, 4);
+  else if (n <= 16) NSP_USE(8, 2, 1, 2);
+  else if (n <= 32) NSP_USE(16, 2, 1, 2);
+  else if (n <= 64) NSP_USE(32, 2, 1, 2);
+  else if (n <= 128) NSP_USE(32, 4, 1, 2);
+  else if (n <= 256) NSP_USE(32, 4, 2, 2);
+  else if (n <= 512) NSP_USE(32, 4, 4, 2);
+  else if (n <= 1024) {  // one barrier for four warps (bf16, 16,384 rows: 105 us; eight warps of four vectors 116)
+    if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 4, 2);
+    else NSP_USE(32, 4, 8, 2);
   }
+  else NSP_USE(32, 4, 16, 2);
+#undef NSP_USE
   l.blocks = (rows + per_block - 1) / per_block;
   return l;
 }
@@ -848,21 +961,16 @@ Launch bwd_launch(int dim, int64_t rows) {
   else if (n <= 32) brief(norm_bwd_short_kernel<T, 16, 2, 2, kKind>, 16, 2);
   else if (n <= 64) brief(norm_bwd_short_kernel<T, 32, 2, 2, kKind>, 32, 2);
   else {
-    int vecs = 2;
-    if (sizeof(T) == 2) {
-      rows_of_block = n <= 1024 ? 2 : 1;
-      if (n > 1024) vecs = 4, l.kernel = norm_bwd_long_kernel<T, 4, 1, kKind>;
-      else l.kernel = norm_bwd_long_kernel<T, 2, 2, kKind>;
-    } else {
-      rows_of_block = 1;
-      if (n > 1024) vecs = 4, l.kernel = norm_bwd_long_kernel<T, 4, 1, kKind>;
-      else l.kernel = norm_bwd_long_kernel<T, 2, 1, kKind>;
-    }
-    l.threads = round32((n + vecs - 1) / vecs);
-    const int stage = 2 * rows_of_block * l.threads * vecs * 8 * static_cast<int>(sizeof(T));
-    // two blocks an SM where three stages of each fit, or four of short ones
-    const int by_threads = 1024 / l.threads < 4 ? 1024 / l.threads : 4;
-    int per_sm = by_threads;
+    const int vecs = n > 1024 ? 4 : 2;
+    if (n > 1024) l.kernel = norm_bwd_long_kernel<T, 512, 4, kKind>;
+    else if (n > 512) l.kernel = norm_bwd_long_kernel<T, 512, 2, kKind>;
+    else l.kernel = norm_bwd_long_kernel<T, 256, 2, kKind>;
+    l.threads = n > 512 ? 512 : 256;
+    l.team = round32((n + vecs - 1) / vecs);
+    rows_of_block = l.threads / l.team;
+    const int stage = 2 * l.threads * vecs * 8 * static_cast<int>(sizeof(T));
+    // two blocks an SM where three stages of each fit
+    int per_sm = l.threads > 256 ? 1 : 2;
     while (per_sm > 1 && per_sm * (3 * stage + 2048) > kMostShared) --per_sm;
     l.stages = 3;
     while (l.stages > 1 && l.stages * stage + 2048 > kMostShared) --l.stages;
@@ -894,7 +1002,7 @@ cudaError_t launch(const Launch& l, NormArgs& a, cudaStream_t st) {
     const cudaError_t e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.shared);
     if (e != cudaSuccess) return cudaGetLastError(), e;
   }
-  a.stages = l.stages;
+  a.stages = l.stages, a.team = l.team;
   nsp::count_launches(1);
   return nsp::launch_chained_if(true, l.kernel, static_cast<unsigned>(l.blocks), l.threads, l.shared, st, a);
 }

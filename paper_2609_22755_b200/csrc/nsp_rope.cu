@@ -6,13 +6,13 @@
 //
 // The angle. p f reaches 10^5 radians and more, where 32 bits leave two or three digits of the angle. A frequency is therefore
 // kept as a fraction of a turn in 64-bit fixed point, F = round(2^64 frac(f / 2 pi)): p F modulo 2^64 is the exact fractional
-// turn of p F (an integer product drops whole turns by itself), its upper 32 bits as a signed number are the angle within half a
-// turn, 2^-32 of a turn apart, and sincospif takes it from there. The error is p * 2^-65 of a turn, for any p a batch can
-// have below the rounding of the cosine.
+// turn of p F (an integer product drops whole turns by itself). Its upper 32 bits give the quarter turn and, as a signed number,
+// the rest within an eighth; the error is p * 2^-65 of a turn, for any p a batch can have below the rounding of the cosine.
 //
 // Work. A thread owns V pairs of a head (one 16-byte load for each half of them in bf16) of up to 16 neighbouring heads of one
-// token: the sines and cosines are computed once for these, and up to four heads' loads are under way at a time. Groups of J
-// threads, one per slot of a head, cover all slots of a (token, heads) piece.
+// token, or of all heads of q and of k where they are no more (a chain's upper nodes: 4 and 1): the sines and cosines are computed
+// once for these, and up to four heads' loads are under way at a time. Groups of J threads, one per slot of a head, cover all
+// slots of a (token, heads) piece.
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -39,6 +39,7 @@ struct RopeTensor {
   uint32_t tokens;
   int32_t heads, per, chunks;  // `per` heads of a thread, `chunks` such pieces of a token
   int32_t f32;
+  int32_t joined;  // 1: its threads go on with the next tensor's heads of the token; that one has no blocks of its own
 };
 
 struct RopeArgs {
@@ -102,46 +103,63 @@ struct Raw {
   }
 };
 
-template <typename T, int V, bool kHalf>
-__device__ __forceinline__ void rope_piece(const RopeTensor& t, const uint64_t* freq, uint32_t token, int h0, int slot, int rot_slots,
-                                           int dim, int rot, float magnitude, float sin_sign) {
+// m cos and m sin of a turn in 64-bit fixed point (sin_m: m or -m). The rest of the angle behind its quarter turn, f in [-pi/4, pi/4],
+// goes through polynomials in f^2 fitted for the smallest relative error by reweighted least squares (sine 3.8e-9, cosine 1.2e-10);
+// in fp32 both are within 1.7 * 2^-24. A third of the instructions of a general sincospi, which has to find the quarter turn of a
+// float.
+__device__ __forceinline__ void sincos_turn(uint64_t turn, float m, float sin_m, float& c, float& s) {
+  const uint32_t top = static_cast<uint32_t>(turn >> 32), quarter = (top + 0x20000000u) >> 30;
+  const float f = static_cast<float>(static_cast<int32_t>(top - (quarter << 30))) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+  const float f2 = f * f;
+  float p = fmaf(f2, -0.00019515282684585036f, 0.00833216075923622f);
+  p = fmaf(p, f2, -0.16666654609533538f);
+  const float sine = fmaf(p, f2 * f, f);
+  float q = fmaf(f2, 2.4433155139662247e-05f, -0.0013887316236525606f);
+  q = fmaf(q, f2, 0.041666645682576074f);
+  q = fmaf(q, f2, -0.5f);
+  const float cosine = fmaf(q, f2, 1.f);
+  const bool odd = quarter & 1;
+  const float u = odd ? sine : cosine, v = odd ? cosine : sine;
+  // quarter 0: (cos, sin), 1: (-sin, cos), 2: (-cos, -sin), 3: (sin, -cos)
+  c = __uint_as_float(__float_as_uint(u) ^ (((quarter + 1) & 2) << 30)) * m;
+  s = __uint_as_float(__float_as_uint(v) ^ ((quarter & 2) << 30)) * sin_m;
+}
+
+// What a thread has of every head: the two vectors of its slot, V first and V second elements of pairs, or V pairs of neighbours; or
+// two vectors of the rest, copied.
+template <int V, bool kHalf>
+struct Slot {
+  int a_at, b_at;
+  bool rotates, second;
+  __device__ __forceinline__ Slot(int slot, int rot_slots, int dim, int rot) : rotates(slot < rot_slots), second(true) {
+    if (rotates) {
+      a_at = kHalf ? slot * V : 2 * slot * V;
+      b_at = kHalf ? rot / 2 + slot * V : (2 * slot + 1) * V;
+    } else {
+      a_at = rot + 2 * (slot - rot_slots) * V;
+      b_at = a_at + V;
+      second = b_at < dim;
+    }
+  }
+};
+
+template <typename T, int V, bool kHalf, typename Angles>
+__device__ __forceinline__ void rope_heads(const RopeTensor& t, uint32_t token, int h0, int n, const Slot<V, kHalf>& at, const float (&c)[V],
+                                           const float (&s)[V], Angles angles) {
   constexpr int kBatch = V * sizeof(T) > 16 ? 2 : 4;  // heads whose loads are under way together
-  const int n = min(t.per, t.heads - h0);
   const T* x = static_cast<const T*>(t.x) + static_cast<int64_t>(token) * t.x_tok + h0 * t.x_head;
   T* y = static_cast<T*>(t.y) + static_cast<int64_t>(token) * t.y_tok + h0 * t.y_head;
-  // the two vectors of a slot: V first and V second elements of pairs, or V pairs of neighbours; two vectors of the rest
-  const bool rotates = slot < rot_slots;
-  int a_at, b_at;
-  bool second = true;
-  if (rotates) {
-    a_at = kHalf ? slot * V : 2 * slot * V;
-    b_at = kHalf ? rot / 2 + slot * V : (2 * slot + 1) * V;
-  } else {
-    a_at = rot + 2 * (slot - rot_slots) * V;
-    b_at = a_at + V;
-    second = b_at < dim;
-  }
-  const uint64_t p = t.pos ? static_cast<uint64_t>(t.pos[token]) : token;
-  float c[V], s[V];
   for (int first = 0; first < n; first += kBatch, x += kBatch * t.x_head, y += kBatch * t.y_head) {
     Raw<T, V> a[kBatch], b[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (first + i < n) {
-        a[i].load(x + i * t.x_head + a_at);
-        if (second) b[i].load(x + i * t.x_head + b_at);
+        a[i].load(x + i * t.x_head + at.a_at);
+        if (at.second) b[i].load(x + i * t.x_head + at.b_at);
       }
     }
-    if (rotates) {
-      if (first == 0) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int32_t turn = static_cast<int32_t>((p * freq[slot * V + i]) >> 32);
-          sincospif(static_cast<float>(turn) * 0x1p-31f, &s[i], &c[i]);
-          c[i] *= magnitude;
-          s[i] *= sin_sign;
-        }
-      }
+    if (at.rotates) {
+      if (first == 0) angles();  // while the first loads are under way
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
         float u[V], v[V];
@@ -166,8 +184,8 @@ __device__ __forceinline__ void rope_piece(const RopeTensor& t, const uint64_t* 
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (first + i < n) {
-        a[i].store(y + i * t.y_head + a_at);
-        if (second) b[i].store(y + i * t.y_head + b_at);
+        a[i].store(y + i * t.y_head + at.a_at);
+        if (at.second) b[i].store(y + i * t.y_head + at.b_at);
       }
     }
   }
@@ -189,10 +207,21 @@ __global__ void __launch_bounds__(V == 1 ? 512 : 256, V == 1 ? 1 : kF32 ? 2 : 3)
   if (group >= static_cast<int64_t>(t.tokens) * t.chunks) return;
   const uint32_t token = static_cast<uint32_t>(group) / static_cast<uint32_t>(t.chunks);  // groups of a tensor: below 2^32
   const int h0 = static_cast<int>(static_cast<uint32_t>(group) - token * t.chunks) * t.per;
-  if (kF32 && t.f32)
-    rope_piece<float, V, kHalf>(t, freq, token, h0, slot, a.rot_slots, a.dim, a.rot, a.magnitude, a.sin_sign);
-  else
-    rope_piece<__nv_bfloat16, V, kHalf>(t, freq, token, h0, slot, a.rot_slots, a.dim, a.rot, a.magnitude, a.sin_sign);
+  const Slot<V, kHalf> at(slot, a.rot_slots, a.dim, a.rot);
+  const uint64_t p = t.pos ? static_cast<uint64_t>(t.pos[token]) : token;
+  float c[V], s[V];
+  auto angles = [&]() {
+#pragma unroll
+    for (int i = 0; i < V; ++i) sincos_turn(p * freq[slot * V + i], a.magnitude, a.sin_sign, c[i], s[i]);
+  };
+  auto heads = [&](const RopeTensor& t, int h0, auto first) {
+    if (kF32 && t.f32)
+      rope_heads<float, V, kHalf>(t, token, h0, min(t.per, t.heads - h0), at, c, s, first);
+    else
+      rope_heads<__nv_bfloat16, V, kHalf>(t, token, h0, min(t.per, t.heads - h0), at, c, s, first);
+  };
+  heads(t, h0, angles);
+  if (t.joined) heads(a.t[k + 1], 0, [] {});
 }
 
 // Rows [tokens, heads] of `dim` elements at these strides do not overlap.
@@ -311,7 +340,12 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
     t.per = per < t.heads ? per : t.heads;
     t.chunks = (t.heads + t.per - 1) / t.per;
     t.block0 = blocks;
-    blocks += (static_cast<int64_t>(t.tokens) * t.chunks + a.per_block - 1) / a.per_block;
+    t.joined = 0;
+    if (i > 0 && per == kMostHeads && !a.t[i - 1].joined && a.t[i - 1].pos == t.pos && a.t[i - 1].tokens == t.tokens &&
+        (i < 2 || !a.t[i - 2].joined) && a.t[i - 1].heads + t.heads <= kMostHeads)
+      a.t[i - 1].joined = 1;
+    else
+      blocks += (static_cast<int64_t>(t.tokens) * t.chunks + a.per_block - 1) / a.per_block;
   }
   if (blocks > INT32_MAX) return NSP_ERR_UNSUPPORTED;
   const bool half = layout == NSP_ROPE_HALF;
