@@ -53,6 +53,7 @@ struct Problem {
   int32_t a_map[2], b_map[2][2];     // [segment], [segment][rank of the CTA]: first of an operand's two maps
   int32_t a_mn, b_mn;                // 1: the contiguous index is the row / column one
   int32_t b_shared;                  // 1: both CTAs' parts of B come from one matrix, nh columns apart
+  int32_t splits, per_split, part;   // a tile's contraction in `splits` parts of per_split stages, partial tiles from `part` on
   int32_t rows, cols;                // of the output
   int32_t out_map;                   // forward: of h, g, u
   __nv_bfloat16* out[3];
@@ -85,6 +86,7 @@ struct GemmArgs {
   int32_t n_problems, nh;
   Schedule order;
   StatusWord status;
+  float* partial;  // [partial tile][CTA][4 columns][128 rows][4]: accumulators of tiles whose contraction is split
 };
 
 struct Maps {
@@ -126,10 +128,11 @@ __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
   }
 }
 
-// The tiles of a problem: kGroup row tiles at a time, over all column tiles, so that the tiles under way at one time share
+// The tiles of a problem, the parts of a tile one after the other: kGroup row tiles at a time, over all column tiles, so that the tiles under way at one time share
 // both their rows and their columns in L2.
 template <int kGroup>
 __device__ __forceinline__ void tile_at(const Problem& p, int tile, int& m, int& n) {
+  tile /= p.splits;
   const int per_group = kGroup * p.tiles_n, group = tile / per_group, rest = tile - group * per_group;
   const int first = group * kGroup, size = min(kGroup, p.tiles_m - first);
   n = rest / size;
@@ -164,6 +167,16 @@ __device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* ma
     for (int c = 0; c < last; c += 64) tma_load_2d_pair(dst + c / 64 * block, maps + 1, bar, at + c, other);
   }
 }
+// The stages of one part of a tile's contraction.
+struct Part {
+  int first, last;
+  __device__ __forceinline__ Part(const Problem& p, int tile) {
+    const int all = p.segments * p.k_iters;
+    first = tile % p.splits * p.per_split;
+    last = min(first + p.per_split, all);
+  }
+};
+
 template <int kDepth>
 __device__ __forceinline__ uint32_t operand_bytes(int mn, int wide, int k, int k_end) {
   return mn || k + 64 < k_end ? wide * kDepth * 2 : wide * 64 * 2;
@@ -278,21 +291,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         const int mine = static_cast<int>(rank);
         const int across = is_a ? m * kTileRows + mine * G::kRows : p.b_shared ? n * 2 * nh + mine * nh : n * nh;
         const int mn = is_a ? p.a_mn : p.b_mn, wide = is_a ? G::kRows : nh, end = is_a ? p.rows : p.cols;
-        for (int seg = 0; seg < p.segments && ok; ++seg) {
-          const CUtensorMap* map = &maps.m[is_a ? p.a_map[seg] : p.b_map[seg][mine]];
-          for (int k = 0; k < p.k_iters; ++k, ++it) {
-            const uint32_t st = it % kStages, ph = (it / kStages) & 1;
-            if (*abort_flag || !mbar_wait(&s.empty[st], ph ^ 1, kWaitLimit)) {
-              if (!*abort_flag) report_timeout(a.status, tile, kWhereGluEmpty, k);
-              raise_abort();
-              ok = false;
-              break;
-            }
-            if (is_a && rank == 0)
-              mbar_expect_tx(&s.full[st], 2 * (operand_bytes<kDepth>(p.a_mn, G::kRows, k * kDepth, p.depth) +
-                                               operand_bytes<kDepth>(p.b_mn, nh, k * kDepth, p.depth)));
-            load_operand<kDepth>(is_a ? stage_a(st) : stage_b(st), map, lead + off(&s.full[st]), mn, across, k * kDepth, wide, end, p.depth);
+        const CUtensorMap* const map0 = &maps.m[is_a ? p.a_map[0] : p.b_map[0][mine]];
+        const CUtensorMap* const map1 = &maps.m[is_a ? p.a_map[1] : p.b_map[1][mine]];  // of the second segment
+        const Part part(p, tile - p.first_tile);
+        for (int k = part.first; k < part.last; ++k, ++it) {
+          const uint32_t st = it % kStages, ph = (it / kStages) & 1;
+          if (*abort_flag || !mbar_wait(&s.empty[st], ph ^ 1, kWaitLimit)) {
+            if (!*abort_flag) report_timeout(a.status, tile, kWhereGluEmpty, k);
+            raise_abort();
+            ok = false;
+            break;
           }
+          const bool second = k >= p.k_iters;
+          const int at = (second ? k - p.k_iters : k) * kDepth;
+          if (is_a && rank == 0)
+            mbar_expect_tx(&s.full[st], 2 * (operand_bytes<kDepth>(p.a_mn, G::kRows, at, p.depth) + operand_bytes<kDepth>(p.b_mn, nh, at, p.depth)));
+          load_operand<kDepth>(is_a ? stage_a(st) : stage_b(st), second ? map1 : map0, lead + off(&s.full[st]), mn, across, at, wide, end, p.depth);
         }
       }
     }
@@ -310,7 +324,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       // 16 steps of the contraction: 32 bytes of a row (four of them in a block), or 16 rows
       const uint32_t a_lbo = p.a_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : G::kRows * 8;
       const uint32_t b_lbo = p.b_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
-      const int iters = p.segments * p.k_iters;
+      const Part part(p, tile - p.first_tile);
+      const int iters = part.last - part.first;
       auto acc_free = [&](uint32_t which) -> bool {
         const bool here = cluster_wait_tmem(&s.acc_empty[which], turn ^ 1, kWaitLimit);
         if (!__all_sync(0xffffffffu, here)) {
@@ -333,7 +348,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       };
       auto issue = [&](int k, uint32_t half, bool last_use) {
         const uint32_t st = (it + k) % kStages;
-        const int left = p.depth - (k >= p.k_iters ? k - p.k_iters : k) * kDepth;  // steps of the segment from this stage on
+        const int at = part.first + k;
+        const int left = p.depth - (at >= p.k_iters ? at - p.k_iters : at) * kDepth;  // steps of the segment from this stage on
         if (leader) {
           const uint32_t a_lo = (smem_desc_addr(stage_a(st)) + half * (kBlock >> 4)) | a_lbo, b_lo = smem_desc_addr(stage_b(st)) | b_lbo;
 #pragma unroll
@@ -449,6 +465,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
           }
           drained();
         }
+      } else if (p.splits > 1) {
+        // fp32, four columns of 128 rows side by side: a warp writes 512 contiguous bytes at a time
+        float* const to = a.partial + (static_cast<int64_t>(p.part + tile - p.first_tile) * 2 + rank) * 256 * nh;
+        for (int c = half * nh; c < (half + 1) * nh; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(t0 + c, r);
+          tmem_wait_ld();
+          if (c + 32 >= (half + 1) * nh) drained();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(to + ((c / 4 + i) * 128 + thread) * 4) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+        }
       } else {
         // nh columns a warpgroup, 64 at a time
         for (int c = 0; c < nh; c += 64) {
@@ -477,6 +505,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
   tc_fence_before_sync();
   cluster_sync();  // neither CTA leaves while the other may still reach its shared memory or issue products into its TMEM
   if (warp == 0) tmem_dealloc_pair(s.tmem_base, 512);
+}
+
+// The outputs of problems whose contraction is split: the parts of a tile added in their order. A block has 32 columns of a CTA's
+// 128 rows.
+struct SumArgs {
+  Problem p[kMostProblems];
+  int32_t n_problems, nh;
+  const float* partial;
+};
+__global__ void __launch_bounds__(256) glu_sum_kernel(const __grid_constant__ SumArgs a) {
+  grid_wait_predecessor();
+  grid_launch_dependents();
+  const int groups = a.nh / 16;  // of 32 columns
+  int tile = static_cast<int>(blockIdx.x) / (2 * groups), k = 0;
+  while (k + 1 < a.n_problems && tile >= a.p[k].tiles_m * a.p[k].tiles_n) tile -= a.p[k].tiles_m * a.p[k].tiles_n, ++k;
+  const Problem& p = a.p[k];
+  const int rest = static_cast<int>(blockIdx.x) % (2 * groups), rank = rest / groups, group = rest % groups;
+  int m, n;
+  tile_at<kGroupM>(p, tile * p.splits, m, n);
+  const int64_t size = 256 * a.nh;
+  const float* from = a.partial + (static_cast<int64_t>(p.part + tile * p.splits) * 2 + rank) * size;
+  const int thread = threadIdx.x & 127, row = m * 256 + rank * 128 + thread;
+  if (row >= p.rows) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = group * 32 + (2 * i + (threadIdx.x >> 7)) * 8, col = n * 2 * a.nh + c;
+    if (col >= p.cols) continue;
+    float4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
+    const float* q = from + (c / 4 * 128 + thread) * 4;
+#pragma unroll 4
+    for (int part = 0; part < p.splits; ++part, q += 2 * size) {
+      const float4 u = *reinterpret_cast<const float4*>(q), v = *reinterpret_cast<const float4*>(q + 512);
+      x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
+      y.x += v.x, y.y += v.y, y.z += v.z, y.w += v.w;
+    }
+    *reinterpret_cast<uint4*>(p.out[0] + row * p.ld[0] + col) =
+        make_uint4(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w), pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+  }
 }
 
 // dg and du, 8 values a thread and access. HBM-bound: three reads and two writes of 2 bytes a value.
@@ -585,29 +651,29 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 // latest end. (4,099 tokens, 2,056 x 5,512 backward: 153 tiles of 88 stages and 396 of 33; the latest pair has 429 stages where all
 // tiles are dealt out one by one, 374 so, of a mean of 359.)
 Schedule plan_schedule(int n_long, int cost, int n_short, int less, int pairs, int64_t* latest) {
-  Schedule best{n_long, n_short, n_long % pairs, 0, 0};
-  *latest = static_cast<int64_t>((n_long + pairs - 1) / pairs) * cost;
+  const int heavy = n_long % pairs, light = pairs - heavy, rounds = n_long / pairs;
+  Schedule best{n_long, n_short, heavy, 0, 0};
+  *latest = static_cast<int64_t>(rounds + (heavy > 0)) * cost;
   if (n_short == 0) return best;
   int64_t best_end = -1;
-  const int most = best.heavy ? (cost + less - 1) / less : 0;
-  for (int ahead = 0; ahead <= most; ++ahead) {
-    for (int start : {0, best.heavy}) {
-      const Schedule s{n_long, n_short, best.heavy, ahead, start};
-      int64_t end = 0;
-      const int light = pairs - s.heavy, rest = n_short - ahead * light;  // of the rounds that all pairs take part in
-      for (int pair = 0; pair < pairs; ++pair) {
-        int64_t n;
-        if (rest <= 0) {
-          n = pair < s.heavy ? 0 : n_short / light + (pair - s.heavy < n_short % light ? 1 : 0);
-        } else {
-          const int at = pair >= start ? pair - start : pair - start + pairs;
-          n = (pair < s.heavy ? 0 : ahead) + rest / pairs + (at < rest % pairs ? 1 : 0);
-        }
-        const int64_t load = static_cast<int64_t>(n_long / pairs + (pair < s.heavy ? 1 : 0)) * cost + n * less;
-        end = load > end ? load : end;
+  const int level = heavy ? cost / less : 0;  // rounds ahead that even out what the heavy pairs have more
+  for (int ahead = level > 1 ? level - 1 : 0; ahead <= level + 1; ++ahead) {
+    for (int start : {0, heavy}) {
+      const int64_t rest = n_short - static_cast<int64_t>(ahead) * light;  // of the rounds that all pairs take part in
+      int64_t of_heavy = 0, of_light;
+      if (rest <= 0) {
+        of_light = (n_short + light - 1) / light;
+      } else {
+        const int64_t more = rest % pairs;  // pairs with one more, from `start` on
+        of_heavy = rest / pairs + (more > (start == 0 ? 0 : light));
+        of_light = ahead + rest / pairs + (more > (start == 0 ? heavy : 0));
       }
-      if (best_end < 0 || end < best_end) best = s, best_end = end;
+      const int64_t a = heavy ? static_cast<int64_t>(rounds + 1) * cost + of_heavy * less : 0;
+      const int64_t b = static_cast<int64_t>(rounds) * cost + of_light * less;
+      if (best_end < 0 || (a > b ? a : b) < best_end) best = Schedule{n_long, n_short, heavy, ahead, start}, best_end = a > b ? a : b;
+      if (!heavy) break;
     }
+    if (!heavy) break;
   }
   *latest = best_end;
   return best;
@@ -626,10 +692,10 @@ cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, bool tall, int pair
 // Sizes of a launch's tiles.
 struct Tiling {
   bool tall;
-  int rows, depth, pairs;  // rows of a tile, steps of a stage
+  int rows, depth, nh, pairs;  // rows of a tile, steps of a stage, columns of a CTA's part of B
   Schedule order;
+  int stages(int64_t steps) const { return static_cast<int>((steps + depth - 1) / depth); }
 };
-Tiling tiling(bool tall) { return Tiling{tall, tall ? 512 : 256, tall ? Geometry<true>::kDepth : Geometry<false>::kDepth, 0, {}}; }
 
 // A matrix of `rows` rows: address and row stride a TMA copy can take, and rows that do not overlap
 int check(const nsp_matrix_t* t, int64_t rows, int64_t cols) {
@@ -640,14 +706,18 @@ int check(const nsp_matrix_t* t, int64_t rows, int64_t cols) {
 }
 int64_t ld_of(const nsp_matrix_t* t, int64_t rows, int64_t cols) { return rows > 1 ? t->row_stride : cols; }
 
-// Tall tiles where they end the launch earlier, a tall one taken as kTallCost of two flat ones. latest(t) plans the order for t and
-// says how many steps of the contraction the pair with most of them has.
-constexpr double kTallCost = 0.95;
+// The tiles that end a launch earliest. end(t) plans the order for t and says how many steps of the contraction the pair with most
+// work has, kStart steps added for every tile. A step of a tall tile takes kTallStep of a flat one's, one of a flat tile with half the
+// columns kNarrowStep (both A and the tensor core's pace stay). Measured: tall 2 * 0.93 beside flat tiles with K of 16,384, and no gain
+// with 4,096, where a tile's start, the wait for the epilogue, is a tenth of it.
+constexpr int kStartFlat = 128, kStartTall = 512;
+constexpr double kTallStep = 1.86, kNarrowStep = 0.65;
 template <typename F>
-Tiling choose_tiling(F latest) {
-  Tiling flat = tiling(false), tall = tiling(true);
-  const int64_t end_flat = latest(flat), end_tall = latest(tall);
-  return 2 * kTallCost * end_tall <= end_flat ? tall : flat;
+Tiling choose_tiling(F end) {
+  Tiling flat{false, 256, Geometry<false>::kDepth, 128, 0, {}}, tall{true, 512, Geometry<true>::kDepth, 128, 0, {}}, narrow = flat;
+  narrow.nh = 64;
+  const double by_flat = end(flat, kStartFlat), by_tall = kTallStep * end(tall, kStartTall), by_narrow = kNarrowStep * end(narrow, kStartFlat);
+  return by_tall <= by_flat && by_tall <= by_narrow ? tall : by_narrow < by_flat ? narrow : flat;
 }
 
 int check_sizes(int64_t rows, int32_t d_model, int32_t d_ff, int32_t act) {
@@ -675,18 +745,18 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
   if ((rc = record_of(&rec)) != NSP_OK) return rc;
   GemmArgs a = {};
   Maps maps;
-  a.nh = 128;
   Problem& p = a.p[0];
-  p.tiles_n = ceil_div(d_ff, a.nh);
-  const Tiling t = choose_tiling([&](Tiling& t) {
-    const int n = ceil_div(T, t.rows) * p.tiles_n;
-    t.pairs = n < rec->sms / 2 ? n : rec->sms / 2;
+  const int most = rec->sms / 2;
+  const Tiling t = choose_tiling([&](Tiling& t, int start) {
+    const int n = ceil_div(T, t.rows) * ceil_div(d_ff, t.nh);
+    t.pairs = n < most ? n : most;
     int64_t latest;
-    t.order = plan_schedule(n, ceil_div(d_model, t.depth) * t.depth, 0, 0, t.pairs, &latest);
+    t.order = plan_schedule(n, t.stages(d_model) * t.depth + start, 0, 0, t.pairs, &latest);
     return latest;
   });
-  p.tiles_m = ceil_div(T, t.rows);
-  p.segments = 1, p.depth = d_model, p.k_iters = ceil_div(d_model, t.depth);
+  a.nh = t.nh;
+  p.tiles_m = ceil_div(T, t.rows), p.tiles_n = ceil_div(d_ff, t.nh);
+  p.segments = 1, p.depth = d_model, p.k_iters = p.per_split = t.stages(d_model), p.splits = 1;
   p.a_map[0] = 0, p.b_map[0][0] = 2, p.b_map[0][1] = 4, p.out_map = 6;
   p.rows = T, p.cols = d_ff;
   const nsp_matrix_t* outs[3] = {h, g, u};
@@ -708,11 +778,18 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
              ? NSP_OK : NSP_ERR_CUDA;
 }
 
+namespace {
+size_t activation_bytes(int64_t rows, int32_t d_ff) { return (2 * 2 * static_cast<size_t>(rows) * d_ff + 255) / 256 * 256; }
+// Partial tiles of split contractions: no more than kMostPartial tiles of 256 x 256 fp32
+constexpr int kMostPartial = 96;
+constexpr size_t kPartialBytes = static_cast<size_t>(kMostPartial) * 256 * 256 * 4;
+}  // namespace
+
 extern "C" int nsp_glu_bwd_ws_bytes(int64_t rows, int32_t d_model, int32_t d_ff, size_t* bytes) {
   if (!bytes) return NSP_ERR_INVALID_ARG;
   const int rc = check_sizes(rows, d_model, d_ff, NSP_ACT_SILU);
   if (rc != NSP_OK) return rc;
-  *bytes = 2 * 2 * static_cast<size_t>(rows) * d_ff;
+  *bytes = activation_bytes(rows, d_ff) + kPartialBytes * (rows > 0);
   return NSP_OK;
 }
 
@@ -738,8 +815,9 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
       (want_x && ((rc = check(dx, rows, d_model)) || (rc = check(w_gate, d_ff, d_model)) || (rc = check(w_up, d_ff, d_model)))))
     return rc;
   if (!want_w && !want_x) return NSP_OK;
-  const size_t half = 2 * static_cast<size_t>(rows) * d_ff;
-  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < 2 * half) return NSP_ERR_WORKSPACE;
+  size_t need = 0;
+  nsp_glu_bwd_ws_bytes(rows, d_model, d_ff, &need);
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < need) return NSP_ERR_WORKSPACE;
   DeviceRecord* rec = nullptr;
   if ((rc = record_of(&rec)) != NSP_OK) return rc;
   ActArgs act_args = {};
@@ -750,60 +828,99 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   act_args.per_row = d_ff / 8, act_args.total = static_cast<uint32_t>(rows * (d_ff / 8));
   GemmArgs a = {};
   Maps maps;
-  a.nh = 128;
   bool ok = true;
   // dg, du as [rows, d_ff]: the contraction of dx runs along their rows, that of the weights' gradients along their columns
-  const int tiles_n = ceil_div(d_model, 2 * a.nh);
-  const bool x_first = want_x && 2 * int64_t{d_ff} > rows;  // the longer tiles
-  const Tiling t = choose_tiling([&](Tiling& t) {
-    const int w_tiles = want_w ? 2 * ceil_div(d_ff, t.rows) * tiles_n : 0, x_tiles = want_x ? ceil_div(T, t.rows) * tiles_n : 0;
-    const int w_cost = ceil_div(T, t.depth) * t.depth, x_cost = 2 * ceil_div(d_ff, t.depth) * t.depth;
-    t.pairs = w_tiles + x_tiles < rec->sms / 2 ? w_tiles + x_tiles : rec->sms / 2;
+  const int most = rec->sms / 2;
+  struct Class {  // of tiles: dW or dx
+    int tiles, stages, splits, per_split;
+  };
+  auto classes = [&](const Tiling& t, Class& w, Class& x) {
+    const int tiles_n = ceil_div(d_model, 2 * t.nh);
+    w = Class{want_w ? 2 * ceil_div(d_ff, t.rows) * tiles_n : 0, t.stages(T), 1, t.stages(T)};
+    x = Class{want_x ? ceil_div(T, t.rows) * tiles_n : 0, 2 * t.stages(d_ff), 1, 2 * t.stages(d_ff)};
+    if (t.tall) return;
+    // Where a tile alone takes longer than the pairs' share of all stages, its contraction is split: into parts of that share, of four
+    // stages at least, and no more of them than the workspace holds.
+    const int64_t all = static_cast<int64_t>(w.tiles) * w.stages + static_cast<int64_t>(x.tiles) * x.stages;
+    const int share = static_cast<int>((all + most - 1) / most), part = share < 4 ? 4 : share;
+    for (Class* c : {&w, &x}) {
+      if (c->tiles == 0 || 4 * c->stages <= 5 * part) continue;
+      const int room = kMostPartial / 2 / c->tiles, wanted = (c->stages + part - 1) / part, n = wanted < room ? wanted : room;
+      if (n < 2) continue;
+      c->per_split = (c->stages + n - 1) / n;
+      c->splits = (c->stages + c->per_split - 1) / c->per_split;
+    }
+  };
+  const Tiling t = choose_tiling([&](Tiling& t, int start) {
+    Class w, x;
+    classes(t, w, x);
+    const int n_w = w.tiles * w.splits, n_x = x.tiles * x.splits;
+    const int c_w = w.per_split * t.depth + start, c_x = x.per_split * t.depth + start;
+    t.pairs = n_w + n_x < most ? n_w + n_x : most;
     int64_t latest;
-    t.order = x_first ? plan_schedule(x_tiles, x_cost, w_tiles, w_cost, t.pairs, &latest) : plan_schedule(w_tiles, w_cost, x_tiles, x_cost, t.pairs, &latest);
-    return latest;
+    const bool x_long = n_x > 0 && (n_w == 0 || c_x > c_w);
+    t.order = x_long ? plan_schedule(n_x, c_x, n_w, c_w, t.pairs, &latest) : plan_schedule(n_w, c_w, n_x, c_x, t.pairs, &latest);
+    return latest + (w.splits > 1 || x.splits > 1 ? 1024 : 0);  // one launch more
   });
-  int n_tiles = 0;
-  auto add = [&](int64_t out_rows) -> Problem& {
+  Class w, x_class;
+  classes(t, w, x_class);
+  a.nh = t.nh;
+  int n_tiles = 0, n_partial = 0;
+  auto add = [&](int64_t out_rows, const Class& c, const nsp_matrix_t* out, int out_map) -> Problem& {
     Problem& p = a.p[a.n_problems++];
-    p.tiles_m = ceil_div(out_rows, t.rows), p.tiles_n = tiles_n, p.first_tile = n_tiles;
+    p.tiles_m = ceil_div(out_rows, t.rows), p.tiles_n = ceil_div(d_model, 2 * t.nh), p.first_tile = n_tiles;
     p.rows = static_cast<int32_t>(out_rows), p.cols = d_model, p.b_mn = p.b_shared = 1;
-    n_tiles += p.tiles_m * p.tiles_n;
+    p.splits = c.splits, p.per_split = c.per_split, p.part = n_partial;
+    p.out_map = out_map, p.out[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(out->data)), p.ld[0] = ld_of(out, out_rows, d_model);
+    ok = ok && encode_plain(&maps.m[out_map], out->data, d_model, out_rows, p.ld[0], 128);
+    n_tiles += p.tiles_m * p.tiles_n * c.splits;
+    if (c.splits > 1) n_partial += p.tiles_m * p.tiles_n * c.splits;
     return p;
   };
   auto add_w = [&]() {
     const nsp_matrix_t* outs[2] = {dw_gate, dw_up};
     for (int i = 0; i < 2; ++i) {
-      Problem& p = add(d_ff);
-      p.segments = 1, p.depth = T, p.k_iters = ceil_div(T, t.depth), p.a_mn = 1;
-      p.a_map[0] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = 4, p.out_map = 14 + i;
-      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.depth, t.rows / 2) &&
-           encode_plain(&maps.m[14 + i], outs[i]->data, d_model, d_ff, ld_of(outs[i], d_ff, d_model), 128);
+      Problem& p = add(d_ff, w, outs[i], 14 + i);
+      p.segments = 1, p.depth = T, p.k_iters = t.stages(T), p.a_mn = 1;
+      p.a_map[0] = p.a_map[1] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = p.b_map[1][0] = p.b_map[1][1] = 4;
+      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.depth, t.rows / 2);
     }
-    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), t.depth, a.nh);
+    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), t.depth, t.nh);
   };
   auto add_x = [&]() {
-    Problem& p = add(rows);
-    p.segments = 2, p.depth = d_ff, p.k_iters = ceil_div(d_ff, t.depth), p.out_map = 16;
-    ok = ok && encode_plain(&maps.m[16], dx->data, d_model, rows, ld_of(dx, rows, d_model), 128);
+    Problem& p = add(rows, x_class, dx, 16);
+    p.segments = 2, p.depth = d_ff, p.k_iters = t.stages(d_ff);
     for (int i = 0; i < 2; ++i) {
-      const nsp_matrix_t* w = i ? w_up : w_gate;
+      const nsp_matrix_t* weight = i ? w_up : w_gate;
       p.a_map[i] = 6 + 2 * i, p.b_map[i][0] = p.b_map[i][1] = 10 + 2 * i;
       ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.rows / 2, t.depth) &&
-           encode_operand(&maps.m[10 + 2 * i], w->data, d_model, d_ff, ld_of(w, d_ff, d_model), t.depth, a.nh);
+           encode_operand(&maps.m[10 + 2 * i], weight->data, d_model, d_ff, ld_of(weight, d_ff, d_model), t.depth, t.nh);
     }
   };
-  if (x_first) add_x();
+  const bool x_long = x_class.tiles > 0 && (w.tiles == 0 || x_class.per_split > w.per_split);
+  if (x_long) add_x();
   if (want_w) add_w();
-  if (!x_first && want_x) add_x();
+  if (!x_long && want_x) add_x();
   a.order = t.order;
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + activation_bytes(rows, d_ff));
   if (!ok) return NSP_ERR_CUDA;
   a.status = rec->word;
   count_launches(1);
   const int blocks = act_args.total / 256 + 1 < 148u * 8 ? static_cast<int>(act_args.total / 256 + 1) : 148 * 8;
   if (launch_chained_if(true, act == NSP_ACT_SILU ? glu_act_kernel<kSilu> : glu_act_kernel<kGelu>, blocks, 256, 0, st, act_args) != cudaSuccess)
     return NSP_ERR_CUDA;
-  return launch_gemm<-1>(maps, a, t.tall, t.pairs, st) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
+  if (launch_gemm<-1>(maps, a, t.tall, t.pairs, st) != cudaSuccess) return NSP_ERR_CUDA;
+  SumArgs sum = {};
+  int n_sum = 0;
+  for (int i = 0; i < a.n_problems; ++i) {
+    if (a.p[i].splits == 1) continue;
+    sum.p[sum.n_problems++] = a.p[i];
+    n_sum += a.p[i].tiles_m * a.p[i].tiles_n;
+  }
+  if (n_sum == 0) return NSP_OK;
+  sum.nh = a.nh, sum.partial = a.partial;
+  count_launches(1);
+  return launch_chained_if(true, glu_sum_kernel, n_sum * 2 * (a.nh / 16), 256, 0, st, sum) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }
 
 extern "C" int nsp_glu_status(int32_t out[4]) {

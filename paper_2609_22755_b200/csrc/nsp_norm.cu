@@ -410,7 +410,7 @@ __device__ __forceinline__ void row_of(uint32_t r, int inner, int64_t& o, int& i
 constexpr int fwd_threads(int warps) { return warps > 4 ? 32 * warps : 128; }
 // Blocks an SM the registers are cut to: five where four vectors a lane are under way (2,048: 50 -> 46 us for 32,768 rows), else the
 // compiler's choice (512: 50 us, cut 54).
-constexpr int fwd_blocks(int vecs, int warps) { return vecs != 4 ? 1 : warps <= 4 ? 5 : warps == 8 ? 2 : 1; }
+constexpr int fwd_blocks(int vecs, int warps) { return vecs != 4 ? 0 : warps <= 4 ? 5 : warps == 8 ? 2 : 1; }
 template <typename T, int kLanes, int kVecs, int kWarps, int kRows, bool kLayer>
 __global__ void __launch_bounds__(fwd_threads(kWarps), fwd_blocks(kVecs, kWarps)) norm_fwd_kernel(const NormArgs a) {
   constexpr int kTeam = kLanes * kWarps, kTeams = fwd_threads(kWarps) / kTeam;

@@ -5,14 +5,15 @@
 // read once and written once, 6 flop per pair.
 //
 // The angle. p f reaches 10^5 radians and more, where 32 bits leave two or three digits of the angle. A frequency is therefore
-// kept as a fraction of a turn in 64-bit fixed point, F = round(2^64 frac(f / 2 pi)): p F modulo 2^64 is the exact fractional
+// kept as a fraction of a turn in 64-bit fixed point, F = 2^64 frac(f / 2 pi): p F modulo 2^64 is the exact fractional
 // turn of p F (an integer product drops whole turns by itself). Its upper 32 bits give the quarter turn and, as a signed number,
-// the rest within an eighth; the error is p * 2^-65 of a turn, for any p a batch can have below the rounding of the cosine.
+// the rest within an eighth; the error is p * 2^-63 of a turn, for any p a batch can have below the rounding of the cosine.
 //
 // Work. A thread owns V pairs of a head (one 16-byte load for each half of them in bf16) of up to 16 neighbouring heads of one
 // token, or of all heads of q and of k where they are no more (a chain's upper nodes: 4 and 1): the sines and cosines are computed
 // once for these, and up to four heads' loads are under way at a time. Groups of J threads, one per slot of a head, cover all
 // slots of a (token, heads) piece.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -42,9 +43,11 @@ struct RopeTensor {
   int32_t joined;  // 1: its threads go on with the next tensor's heads of the token; that one has no blocks of its own
 };
 
+// Kernel parameters for up to kTensors tensors and kPairs frequencies: a launch copies them, and the common call needs a twelfth.
+template <int kTensors, int kPairs>
 struct RopeArgs {
-  uint64_t freq[kMaxPairs];  // turns per position, 64-bit fixed point
-  RopeTensor t[NSP_ROPE_MAX_TENSORS];
+  uint64_t freq[kPairs];  // turns per position, 64-bit fixed point
+  RopeTensor t[kTensors];
   int32_t n, pairs;
   int32_t slots, rot_slots, per_block;  // threads of a group, those that rotate, groups of a block
   int32_t dim, rot;
@@ -192,8 +195,8 @@ __device__ __forceinline__ void rope_heads(const RopeTensor& t, uint32_t token, 
 }
 
 // kF32: tensors of either type; otherwise all of them bf16
-template <int V, bool kHalf, bool kF32>
-__global__ void __launch_bounds__(V == 1 ? 512 : 256, V == 1 ? 1 : kF32 ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
+template <int V, bool kHalf, bool kF32, typename Args>
+__global__ void __launch_bounds__(V == 1 ? 512 : 256, V == 1 ? 1 : kF32 ? 2 : 3) rope_kernel(const __grid_constant__ Args a) {
   __shared__ uint64_t freq[kMaxPairs];
   for (int i = threadIdx.x; i < a.pairs; i += blockDim.x) freq[i] = a.freq[i];
   grid_wait_predecessor();
@@ -278,14 +281,15 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
       (layout != NSP_ROPE_HALF && layout != NSP_ROPE_INTERLEAVED) || !std::isfinite(magnitude))
     return NSP_ERR_INVALID_ARG;
   if (n_tensors > NSP_ROPE_MAX_TENSORS || rot_dim > NSP_ROPE_MAX_ROT || head_dim > NSP_ROPE_MAX_HEAD_DIM) return NSP_ERR_UNSUPPORTED;
-  RopeArgs a;
+  RopeArgs<NSP_ROPE_MAX_TENSORS, kMaxPairs> a;
   a.pairs = rot_dim / 2;
   for (int i = 0; i < a.pairs; ++i) {
     if (!std::isfinite(inv_freq[i])) return NSP_ERR_INVALID_ARG;
     // the 64 bits of mantissa of an x87 long double are those of the fixed point
-    const long double turns = static_cast<long double>(inv_freq[i]) / 6.283185307179586476925286766559L;
-    const long double fixed = std::roundl(std::ldexp(turns - std::floor(turns), 64));
-    a.freq[i] = fixed >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(fixed);
+    long double turns = static_cast<long double>(inv_freq[i]) * 0.159154943091895335768883763372514362L;
+    if (turns < 0 || turns >= 1) turns -= std::floor(turns);
+    turns *= 18446744073709551616.0L;
+    a.freq[i] = turns >= 18446744073709551615.0L ? 0 : static_cast<uint64_t>(turns);
   }
   int vec = 8;  // elements of a vector, as far as every tensor's addresses allow
   auto fits = [&](int v) { return a.pairs % v == 0 && rot_dim % v == 0 && head_dim % v == 0; };
@@ -349,14 +353,25 @@ extern "C" int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int
   }
   if (blocks > INT32_MAX) return NSP_ERR_UNSUPPORTED;
   const bool half = layout == NSP_ROPE_HALF;
-  auto pick = [&](auto v) {
-    constexpr int V = decltype(v)::value;
-    return any_f32 ? (half ? rope_kernel<V, true, true> : rope_kernel<V, false, true>)
-                   : (half ? rope_kernel<V, true, false> : rope_kernel<V, false, false>);
+  const auto launch = [&](const auto& args) {
+    using Args = std::decay_t<decltype(args)>;
+    auto pick = [&](auto v) -> void (*)(const Args) {
+      constexpr int V = decltype(v)::value;
+      return any_f32 ? (half ? rope_kernel<V, true, true, Args> : rope_kernel<V, false, true, Args>)
+                     : (half ? rope_kernel<V, true, false, Args> : rope_kernel<V, false, false, Args>);
+    };
+    void (*kernel)(const Args) = vec == 8 ? pick(std::integral_constant<int, 8>{})
+                                 : vec == 4 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 1>{});
+    nsp::count_launches(1);
+    return nsp::launch_chained_if(true, kernel, static_cast<unsigned>(blocks), a.slots * a.per_block, 0, static_cast<cudaStream_t>(stream),
+                                  args) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
   };
-  void (*kernel)(const RopeArgs) = vec == 8 ? pick(std::integral_constant<int, 8>{})
-                                   : vec == 4 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 1>{});
-  nsp::count_launches(1);
-  return nsp::launch_chained_if(true, kernel, static_cast<unsigned>(blocks), a.slots * a.per_block, 0, static_cast<cudaStream_t>(stream),
-                                a) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
+  constexpr int kFew = 4, kFewPairs = 64;
+  if (a.n > kFew || a.pairs > kFewPairs) return launch(a);
+  RopeArgs<kFew, kFewPairs> few;
+  std::copy_n(a.freq, a.pairs, few.freq);
+  std::copy_n(a.t, a.n, few.t);
+  few.n = a.n, few.pairs = a.pairs, few.slots = a.slots, few.rot_slots = a.rot_slots, few.per_block = a.per_block;
+  few.dim = a.dim, few.rot = a.rot, few.magnitude = a.magnitude, few.sin_sign = a.sin_sign;
+  return launch(few);
 }

@@ -17,7 +17,7 @@ def B():
 BUF = 1 << 20  # an address that is never dereferenced: every case is refused first, or has nothing to do
 
 
-def _call(B, which, rows=4, d=64, f=128, act=0, ws=1 << 28, ws_bytes=1 << 28, **change):
+def _call(B, which, rows=4, d=64, f=128, act=0, ws=1 << 28, ws_bytes=1 << 30, **change):
     shape = {"x": d, "w_gate": d, "w_up": d, "h": f, "g": f, "u": f, "dh": f, "dx": d, "dw_gate": d, "dw_up": d}
     m = {}
     for i, (name, cols) in enumerate(shape.items()):
@@ -51,14 +51,16 @@ def test_refusals(B, which):
         assert call(dw_gate=None, dw_up=None, dx=None) == B.NSP_OK  # nothing is wanted
         assert call(dh=None) == inv and call(g=None) == inv and call(x=None) == inv and call(w_up=None) == inv
         assert call(rows=0, dw_gate=None, dw_up=None) == B.NSP_OK
-        need = 2 * 2 * 4 * 128
+        need = B.nsp_glu_bwd_ws_bytes(4, 64, 128)
         assert call(ws=None) == B.NSP_ERR_WORKSPACE and call(ws=BUF + 16) == B.NSP_ERR_WORKSPACE
         assert call(ws_bytes=need - 1) == B.NSP_ERR_WORKSPACE
 
 
 def test_workspace_and_status(B):
     assert B.nsp_glu_bwd_ws_bytes(0, 64, 128) == 0
-    assert B.nsp_glu_bwd_ws_bytes(16384, 4096, 12288) == 4 * 16384 * 12288
+    dg_du, partial = 4 * 16384 * 12288, B.nsp_glu_bwd_ws_bytes(1, 8, 8)
+    assert dg_du < B.nsp_glu_bwd_ws_bytes(16384, 4096, 12288) <= dg_du + partial  # a bounded part beside dg and du
+    assert partial < 1 << 26
     for bad in ((-1, 64, 128), (4, 60, 128), (4, 64, 0)):
         with pytest.raises(B.NspError):
             B.nsp_glu_bwd_ws_bytes(*bad)

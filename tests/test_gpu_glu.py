@@ -239,7 +239,7 @@ def test_many_small_calls(B):
     """Launches that follow one another without a wait, of other tile counts and operand layouts."""
     import torch
 
-    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(B.nsp_glu_bwd_ws_bytes(700, 136, 328), dtype=torch.uint8, device="cuda")
     e = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
     sets = []
     for k in range(12):
