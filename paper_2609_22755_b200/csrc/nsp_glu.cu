@@ -32,13 +32,13 @@ namespace {
 // A stage: kDepth steps of the contraction, of kRows rows of A and up to 128 of B.
 template <bool kTall>
 struct Geometry {
-  static constexpr int kDepth = kTall ? 64 : 128, kStages = kTall ? 4 : 3;
+  static constexpr int kDepth = kTall ? 64 : 128, kStages = kTall ? 4 : 3;  // stages of full operands
   static constexpr int kHalves = kTall ? 2 : 1;  // products of 256 rows a stage of B is used for
   static constexpr int kRows = 128 * kHalves;
   static constexpr uint32_t kBytesA = kRows * kDepth * 2, kBytesB = 128 * kDepth * 2;
-  static constexpr uint32_t kBlockMn = kDepth * 128;  // bytes of 64 columns of an MN-major operand
 };
 constexpr uint32_t kOperands = 3 * 64 * 1024;
+constexpr int kMostStages = 8;
 static_assert(Geometry<true>::kStages * (Geometry<true>::kBytesA + Geometry<true>::kBytesB) == kOperands, "stages");
 static_assert(Geometry<false>::kStages * (Geometry<false>::kBytesA + Geometry<false>::kBytesB) == kOperands, "stages");
 constexpr uint32_t kBlock = 128 * 64 * 2;  // bytes of a block of 128 rows x 64 columns
@@ -84,6 +84,10 @@ struct Schedule {
 struct GemmArgs {
   Problem p[kMostProblems];
   int32_t n_problems, nh;
+  // Rows of a box of a K-major A and steps of a box of MN-major operands: 128 and a stage's depth, or fewer where there are no more
+  // rows or steps; what the tensor core reads beyond them are other bytes of shared memory, for rows that are not stored. Bytes of a
+  // stage of A and of B, and how many stages fit.
+  int32_t a_rows, mn_steps, bytes_a, bytes_b, stages;
   Schedule order;
   StatusWord status;
   float* partial;  // [partial tile][CTA][4 columns][128 rows][4]: accumulators of tiles whose contraction is split
@@ -96,8 +100,8 @@ struct Maps {
 struct Smem {
   uint8_t operands[kOperands];  // stages of A, then of B
   uint8_t out[2][kBlock];       // a warpgroup's block of an output on its way to memory
-  uint64_t full[4];             // in the first CTA: the bytes of both
-  uint64_t empty[4];            // in both: the products of the stage have completed
+  uint64_t full[kMostStages];   // in the first CTA: the bytes of both
+  uint64_t empty[kMostStages];  // in both: the products of the stage have completed
   uint64_t acc_full[2];         // in both: an accumulator is complete (tall tiles: both halves, the first barrier)
   uint64_t acc_empty[2];        // in the first CTA: 16 warps have read it
   uint32_t tmem_base;
@@ -152,17 +156,17 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* smem_
                : "memory");
 }
 
-// One operand of a stage. `across` is the index of its rows (columns of the output for B), `k` the step of the contraction, `wide`
-// the rows of this CTA. maps[0] holds whole blocks of 64 contiguous columns, two of them a box: {64, the other index, blocks};
-// maps[1] is the plain matrix, for boxes that the end of the contiguous index cuts: the rest reads as zero.
+// One operand of a stage. `across` is the index of its rows (columns of the output for B), `k` the step of the contraction, `wide` and
+// `steps` the box's extent in them. maps[0] holds whole blocks of 64 contiguous columns, two of them (or more) a box: {64, the other
+// index, blocks}; maps[1] is the plain matrix, for boxes that the end of the contiguous index cuts: the rest reads as zero.
 template <int kDepth>
-__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* maps, uint32_t bar, int mn, int across, int k, int wide,
+__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* maps, uint32_t bar, int mn, int across, int k, int wide, int steps,
                                              int across_end, int k_end) {
   const int at = mn ? across : k, other = mn ? k : across, end = mn ? across_end : k_end, cols = mn ? wide : kDepth;
   if (at + cols <= end) {
     tma_load_3d_pair(dst, maps, bar, 0, other, at / 64);
   } else {
-    const uint32_t block = (mn ? kDepth : wide) * 128;
+    const uint32_t block = (mn ? steps : wide) * 128;
     const int last = mn ? cols : min(cols, end - at);  // the contraction ends in this stage: no blocks behind it
     for (int c = 0; c < last; c += 64) tma_load_2d_pair(dst + c / 64 * block, maps + 1, bar, at + c, other);
   }
@@ -178,8 +182,8 @@ struct Part {
 };
 
 template <int kDepth>
-__device__ __forceinline__ uint32_t operand_bytes(int mn, int wide, int k, int k_end) {
-  return mn || k + 64 < k_end ? wide * kDepth * 2 : wide * 64 * 2;
+__device__ __forceinline__ uint32_t operand_bytes(int mn, int wide, int steps, int k, int k_end) {
+  return mn ? wide * steps * 2 : k + 64 < k_end ? wide * kDepth * 2 : wide * 64 * 2;
 }
 
 // 32 columns of one row
@@ -237,13 +241,13 @@ __device__ __forceinline__ void pack_row(const uint32_t (&r)[32], uint32_t (&w)[
 template <int kAct, bool kTall>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
   using G = Geometry<kTall>;
-  constexpr int kDepth = G::kDepth, kStages = G::kStages, kTileRows = 2 * G::kRows, kGroup = kTall ? kGroupTall : kGroupM;
+  constexpr int kDepth = G::kDepth, kTileRows = 2 * G::kRows, kGroup = kTall ? kGroupTall : kGroupM;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Smem& s = *reinterpret_cast<Smem*>(smem_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   if (tid == 0) {
-    for (int i = 0; i < 4; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
+    for (int i = 0; i < kMostStages; ++i) mbar_init(&s.full[i], 1), mbar_init(&s.empty[i], 1);
     for (int i = 0; i < 2; ++i) mbar_init(&s.acc_full[i], 1), mbar_init(&s.acc_empty[i], 16);
     s.abort = 0;
     fence_mbar_init();
@@ -270,8 +274,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
   }
   const int pairs = static_cast<int>(gridDim.x) / 2, pair = static_cast<int>(blockIdx.x) / 2;
   const int nh = a.nh;
-  auto stage_a = [&](uint32_t st) { return s.operands + st * G::kBytesA; };
-  auto stage_b = [&](uint32_t st) { return s.operands + kStages * G::kBytesA + st * G::kBytesB; };
+  const int stages = a.stages;
+  auto stage_a = [&](uint32_t st) { return s.operands + st * a.bytes_a; };
+  auto stage_b = [&](uint32_t st) { return s.operands + stages * a.bytes_a + st * a.bytes_b; };
+  struct Turn {  // a stage of the ring and the phase of its barriers
+    uint32_t st = 0, ph = 0;
+    __device__ __forceinline__ void next(int stages) {
+      if (++st == static_cast<uint32_t>(stages)) st = 0, ph ^= 1;
+    }
+  };
   auto problem_of = [&](int tile) -> const Problem& {
     int k = 0;
     while (k + 1 < a.n_problems && tile >= a.p[k + 1].first_tile) ++k;
@@ -282,21 +293,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     // ================================================================ TMA producers of A and of B (both CTAs, each its own rows)
     if (lane == 0) {
       const bool is_a = warp == 0;
-      uint32_t it = 0;
+      Turn turn;
       bool ok = true;
       for (int i = 0, tile; ok && (tile = a.order.tile(i, pair, pairs)) >= 0; ++i) {
         const Problem& p = problem_of(tile);
         int m, n;
         tile_at<kGroup>(p, tile - p.first_tile, m, n);
+        // first row of A and column of B of either CTA; one whose rows or columns lie behind the end loads nothing
+        auto row_of = [&](int r) { return m * kTileRows + r * G::kRows; };
+        auto col_of = [&](int r) { return p.b_shared ? n * 2 * nh + r * nh : n * nh; };
         const int mine = static_cast<int>(rank);
-        const int across = is_a ? m * kTileRows + mine * G::kRows : p.b_shared ? n * 2 * nh + mine * nh : n * nh;
-        const int mn = is_a ? p.a_mn : p.b_mn, wide = is_a ? G::kRows : nh, end = is_a ? p.rows : p.cols;
+        const int across = is_a ? row_of(mine) : col_of(mine), end = is_a ? p.rows : p.cols;
+        const int mn = is_a ? p.a_mn : p.b_mn, wide_a = p.a_mn ? G::kRows : a.a_rows, wide = is_a ? wide_a : nh;
+        const int of_a = (row_of(0) < p.rows) + (row_of(1) < p.rows), of_b = (col_of(0) < p.cols) + (col_of(1) < p.cols);
         const CUtensorMap* const map0 = &maps.m[is_a ? p.a_map[0] : p.b_map[0][mine]];
         const CUtensorMap* const map1 = &maps.m[is_a ? p.a_map[1] : p.b_map[1][mine]];  // of the second segment
         const Part part(p, tile - p.first_tile);
-        for (int k = part.first; k < part.last; ++k, ++it) {
-          const uint32_t st = it % kStages, ph = (it / kStages) & 1;
-          if (*abort_flag || !mbar_wait(&s.empty[st], ph ^ 1, kWaitLimit)) {
+        for (int k = part.first; k < part.last; ++k, turn.next(stages)) {
+          if (*abort_flag || !mbar_wait(&s.empty[turn.st], turn.ph ^ 1, kWaitLimit)) {
             if (!*abort_flag) report_timeout(a.status, tile, kWhereGluEmpty, k);
             raise_abort();
             ok = false;
@@ -305,8 +319,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
           const bool second = k >= p.k_iters;
           const int at = (second ? k - p.k_iters : k) * kDepth;
           if (is_a && rank == 0)
-            mbar_expect_tx(&s.full[st], 2 * (operand_bytes<kDepth>(p.a_mn, G::kRows, at, p.depth) + operand_bytes<kDepth>(p.b_mn, nh, at, p.depth)));
-          load_operand<kDepth>(is_a ? stage_a(st) : stage_b(st), second ? map1 : map0, lead + off(&s.full[st]), mn, across, at, wide, end, p.depth);
+            mbar_expect_tx(&s.full[turn.st], of_a * operand_bytes<kDepth>(p.a_mn, wide_a, a.mn_steps, at, p.depth) +
+                                                 of_b * operand_bytes<kDepth>(p.b_mn, nh, a.mn_steps, at, p.depth));
+          if (across < end)
+            load_operand<kDepth>(is_a ? stage_a(turn.st) : stage_b(turn.st), second ? map1 : map0, lead + off(&s.full[turn.st]), mn, across, at,
+                                 wide, a.mn_steps, end, p.depth);
         }
       }
     }
@@ -315,15 +332,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
     // ================================================================ issuer of the products, for both CTAs
     const bool leader = elect_one();
     const uint32_t hi = static_cast<uint32_t>(make_smem_desc_sw128(0, 16, 1024) >> 32);
-    uint32_t it = 0, n_done = 0;
+    Turn turn_in;  // of the stage issued next
+    uint32_t n_done = 0;
     bool ok = true;
     for (int tile; ok && (tile = a.order.tile(static_cast<int>(n_done), pair, pairs)) >= 0; ++n_done) {
       const Problem& p = problem_of(tile);
       const uint32_t buf = kTall ? 0 : n_done & 1, turn = kTall ? n_done & 1 : (n_done >> 1) & 1;
       const uint32_t idesc = make_idesc_bf16(256, 2 * nh, p.a_mn, p.b_mn);
       // 16 steps of the contraction: 32 bytes of a row (four of them in a block), or 16 rows
-      const uint32_t a_lbo = p.a_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : G::kRows * 8;
-      const uint32_t b_lbo = p.b_mn ? (G::kBlockMn >> 4) << 16 : 1u << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
+      const uint32_t mn_block = a.mn_steps * 8;  // in units of 16 bytes: 64 columns of an MN-major operand
+      const uint32_t a_lbo = (p.a_mn ? mn_block : 1u) << 16, a_step = p.a_mn ? 128 : 2, a_next = p.a_mn ? 512 : a.a_rows * 8;
+      const uint32_t a_half = p.a_mn ? 2 * mn_block : kBlock >> 4;  // 128 rows on
+      const uint32_t b_lbo = (p.b_mn ? mn_block : 1u) << 16, b_step = p.b_mn ? 128 : 2, b_next = p.b_mn ? 512 : nh * 8;
       const Part part(p, tile - p.first_tile);
       const int iters = part.last - part.first;
       auto acc_free = [&](uint32_t which) -> bool {
@@ -335,9 +355,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         tc_fence_after_sync();
         return true;
       };
-      auto arrived = [&](int k) -> bool {
-        const uint32_t at = it + k;
-        const bool here = *abort_flag == 0 && cluster_wait(&s.full[at % kStages], (at / kStages) & 1, kWaitLimit);
+      auto arrived = [&](int k, const Turn& at) -> bool {
+        const bool here = *abort_flag == 0 && cluster_wait(&s.full[at.st], at.ph, kWaitLimit);
         if (!__all_sync(0xffffffffu, here)) {
           if (lane == 0 && !*abort_flag) report_timeout(a.status, tile, kWhereGluFull, k);
           if (lane == 0) raise_abort();
@@ -346,12 +365,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         tc_fence_after_sync();
         return true;
       };
-      auto issue = [&](int k, uint32_t half, bool last_use) {
-        const uint32_t st = (it + k) % kStages;
+      auto issue = [&](int k, uint32_t st, uint32_t half, bool last_use) {
         const int at = part.first + k;
         const int left = p.depth - (at >= p.k_iters ? at - p.k_iters : at) * kDepth;  // steps of the segment from this stage on
         if (leader) {
-          const uint32_t a_lo = (smem_desc_addr(stage_a(st)) + half * (kBlock >> 4)) | a_lbo, b_lo = smem_desc_addr(stage_b(st)) | b_lbo;
+          const uint32_t a_lo = (smem_desc_addr(stage_a(st)) + half * a_half) | a_lbo, b_lo = smem_desc_addr(stage_b(st)) | b_lbo;
 #pragma unroll
           for (int kk = 0; kk < kDepth / 16; ++kk) {
             if (kk * 16 < left)
@@ -366,23 +384,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       ok = acc_free(buf);
       int k = 0;
       if constexpr (kTall) {
-        const int lead_in = min(kStages, iters);
-        for (; ok && k < lead_in; ++k) {
-          ok = arrived(k);
-          if (ok) issue(k, 0, false);
+        const int lead_in = min(stages, iters);
+        Turn ahead = turn_in;
+        for (; ok && k < lead_in; ++k, ahead.next(stages)) {
+          ok = arrived(k, ahead);
+          if (ok) issue(k, ahead.st, 0, false);
         }
         ok = ok && acc_free(1);
         if (ok) {
-          for (k = 0; k < lead_in; ++k) issue(k, 1, true);
+          for (k = 0; k < lead_in; ++k, turn_in.next(stages)) issue(k, turn_in.st, 1, true);
         }
       }
-      for (; ok && k < iters; ++k) {
-        ok = arrived(k);
+      for (; ok && k < iters; ++k, turn_in.next(stages)) {
+        ok = arrived(k, turn_in);
         if (!ok) break;
-        issue(k, 0, !kTall);
-        if constexpr (kTall) issue(k, 1, true);
+        issue(k, turn_in.st, 0, !kTall);
+        if constexpr (kTall) issue(k, turn_in.st, 1, true);
       }
-      it += iters;
     }
   } else if (warp >= 4) {
     // ================================================================ epilogue: a warpgroup has half of the columns
@@ -449,19 +467,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
             out.end(&maps.m[p.out_map + 2], col, row0, p);
           }
         } else {
-          const int per = nh / 2;  // columns of h of this warpgroup
-          for (int c = half * per; c < (half + 1) * per; c += 32) {
+          const int end = min(p.cols, n * nh + nh);  // a chunk may reach into the next tile's columns
+          for (int c = half * 32; c < nh; c += 64) {
             uint32_t g[32], u[32], w[16];
             tmem_ld32(t0 + c, g);
             tmem_ld32(t0 + nh + c, u);
             tmem_wait_ld();
             const int col = n * nh + c;
-            if (p.out[1]) pack_row(g, w), store_row(p.out[1], p.ld[1], row, col, p.rows, p.cols, w);
-            if (p.out[2]) pack_row(u, w), store_row(p.out[2], p.ld[2], row, col, p.rows, p.cols, w);
+            if (p.out[1]) pack_row(g, w), store_row(p.out[1], p.ld[1], row, col, p.rows, end, w);
+            if (p.out[2]) pack_row(u, w), store_row(p.out[2], p.ld[2], row, col, p.rows, end, w);
 #pragma unroll
             for (int i = 0; i < 32; ++i) g[i] = __float_as_uint(act_value<kAct>(__uint_as_float(g[i])) * __uint_as_float(u[i]));
             pack_row(g, w);
-            store_row(p.out[0], p.ld[0], row, col, p.rows, p.cols, w);
+            store_row(p.out[0], p.ld[0], row, col, p.rows, end, w);
           }
           drained();
         }
@@ -706,18 +724,41 @@ int check(const nsp_matrix_t* t, int64_t rows, int64_t cols) {
 }
 int64_t ld_of(const nsp_matrix_t* t, int64_t rows, int64_t cols) { return rows > 1 ? t->row_stride : cols; }
 
-// The tiles that end a launch earliest. end(t) plans the order for t and says how many steps of the contraction the pair with most
-// work has, kStart steps added for every tile. A step of a tall tile takes kTallStep of a flat one's, one of a flat tile with half the
-// columns kNarrowStep (both A and the tensor core's pace stay). Measured: tall 2 * 0.93 beside flat tiles with K of 16,384, and no gain
-// with 4,096, where a tile's start, the wait for the epilogue, is a tenth of it.
+// The tiles that end a launch earliest. end(t, start) plans the order for t and says how many steps of the contraction the pair with
+// most work has, `start` steps added for every tile. A step of a tall tile takes kTallStep of a flat one's: measured, 2 * 0.93 beside
+// flat tiles with K of 16,384, and no gain with 4,096, where a tile's start, the wait for the epilogue, is a tenth of it. A step of a
+// narrower flat tile takes step(nh) of a full one's: its share of the bytes, a CTA's rows of A and nh columns of B (96 tiles of 128
+// columns on 74 pairs, 128 tokens, 4,096 x 12,288: 55 us, 192 of 64 columns 66; 22 tiles, 77 tokens, 1,024 x 2,816: 11.5 us, 44 of 64
+// columns 8.9). `narrow`: the column counts to try. `tall_too`: enough rows for tall tiles.
 constexpr int kStartFlat = 128, kStartTall = 512;
-constexpr double kTallStep = 1.86, kNarrowStep = 0.65;
-template <typename F>
-Tiling choose_tiling(F end) {
-  Tiling flat{false, 256, Geometry<false>::kDepth, 128, 0, {}}, tall{true, 512, Geometry<true>::kDepth, 128, 0, {}}, narrow = flat;
-  narrow.nh = 64;
-  const double by_flat = end(flat, kStartFlat), by_tall = kTallStep * end(tall, kStartTall), by_narrow = kNarrowStep * end(narrow, kStartFlat);
-  return by_tall <= by_flat && by_tall <= by_narrow ? tall : by_narrow < by_flat ? narrow : flat;
+constexpr double kTallStep = 1.86;
+template <typename Step, typename End>
+Tiling choose_tiling(const int* narrow, int n_narrow, bool tall_too, Step step, End end) {
+  Tiling best{false, 256, Geometry<false>::kDepth, 128, 0, {}};
+  double best_end = static_cast<double>(end(best, kStartFlat));
+  for (int i = 0; i < n_narrow; ++i) {
+    Tiling t{false, 256, Geometry<false>::kDepth, narrow[i], 0, {}};
+    const double e = step(narrow[i]) * end(t, kStartFlat);
+    if (e < best_end) best = t, best_end = e;
+  }
+  if (tall_too) {
+    Tiling t{true, 512, Geometry<true>::kDepth, 128, 0, {}};
+    if (kTallStep * end(t, kStartTall) <= best_end) best = t;
+  }
+  return best;
+}
+
+// Boxes, bytes and number of the stages (see GemmArgs). a_rows: rows there are for a K-major A; mn_steps: the longest contraction over
+// MN-major operands, mn: whether A is one of them in any problem.
+void set_stages(GemmArgs& a, const Tiling& t, int64_t a_rows, int64_t mn_steps, bool a_kmajor, bool a_mn, bool b_mn) {
+  const int full = t.rows / 2;
+  a.a_rows = a_rows < full ? static_cast<int>((a_rows + 7) / 8 * 8) : full;
+  a.mn_steps = mn_steps < t.depth ? static_cast<int>((mn_steps + 15) / 16 * 16) : t.depth;
+  const int k_major = a.a_rows * t.depth * 2, mn = full * a.mn_steps * 2;
+  a.bytes_a = a_mn && (!a_kmajor || mn > k_major) ? mn : k_major;
+  a.bytes_b = a.nh * (b_mn ? a.mn_steps : t.depth) * 2;
+  const int fit = static_cast<int>(kOperands) / (a.bytes_a + a.bytes_b);
+  a.stages = fit < kMostStages ? fit : kMostStages;
 }
 
 int check_sizes(int64_t rows, int32_t d_model, int32_t d_ff, int32_t act) {
@@ -747,7 +788,15 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
   Maps maps;
   Problem& p = a.p[0];
   const int most = rec->sms / 2;
-  const Tiling t = choose_tiling([&](Tiling& t, int start) {
+  // columns that divide d_ff evenly among one to four rounds of all pairs
+  int narrow[4], n_narrow = 0;
+  const int a_box = T < 128 ? T : 128;
+  const int per_round = most / ceil_div(T, 256);
+  for (int round = 1; round <= 4 && per_round > 0; ++round) {
+    const int nh = (ceil_div(d_ff, per_round * round) + 15) / 16 * 16;  // products of a pair have a multiple of 32 columns
+    if (nh < 128) narrow[n_narrow++] = nh < 32 ? 32 : nh;
+  }
+  const Tiling t = choose_tiling(narrow, n_narrow, T > 256, [&](int nh) { return (a_box + nh) / (a_box + 128.0); }, [&](Tiling& t, int start) {
     const int n = ceil_div(T, t.rows) * ceil_div(d_ff, t.nh);
     t.pairs = n < most ? n : most;
     int64_t latest;
@@ -755,6 +804,7 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
     return latest;
   });
   a.nh = t.nh;
+  set_stages(a, t, rows, t.depth, true, false, false);
   p.tiles_m = ceil_div(T, t.rows), p.tiles_n = ceil_div(d_ff, t.nh);
   p.segments = 1, p.depth = d_model, p.k_iters = p.per_split = t.stages(d_model), p.splits = 1;
   p.a_map[0] = 0, p.b_map[0][0] = 2, p.b_map[0][1] = 4, p.out_map = 6;
@@ -766,7 +816,7 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
     p.ld[i] = ld_of(outs[i], rows, d_ff);
     if (!encode_plain(&maps.m[p.out_map + i], outs[i]->data, d_ff, rows, p.ld[i], 128)) return NSP_ERR_CUDA;
   }
-  if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), t.rows / 2, t.depth) ||
+  if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), a.a_rows, t.depth) ||
       !encode_operand(&maps.m[2], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), a.nh, t.depth) ||
       !encode_operand(&maps.m[4], w_up->data, d_model, d_ff, ld_of(w_up, d_ff, d_model), a.nh, t.depth))
     return NSP_ERR_CUDA;
@@ -851,7 +901,9 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
       c->splits = (c->stages + c->per_split - 1) / c->per_split;
     }
   };
-  const Tiling t = choose_tiling([&](Tiling& t, int start) {
+  // Half as many columns: measured, 0.65 a step (1,000 tokens, 1,024 x 2,816: 29.5 us, full tiles 32.5; 77 tokens 16.6 / 18.5)
+  const int half_columns = 64;
+  const Tiling t = choose_tiling(&half_columns, 1, true, [](int) { return 0.65; }, [&](Tiling& t, int start) {
     Class w, x;
     classes(t, w, x);
     const int n_w = w.tiles * w.splits, n_x = x.tiles * x.splits;
@@ -865,6 +917,8 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   Class w, x_class;
   classes(t, w, x_class);
   a.nh = t.nh;
+  // dx contracts over d_ff, its weights MN-major; where it is wanted, that is the longest contraction over MN-major operands
+  set_stages(a, t, rows, want_x && (!want_w || d_ff > T) ? d_ff : T, want_x, want_w, true);
   int n_tiles = 0, n_partial = 0;
   auto add = [&](int64_t out_rows, const Class& c, const nsp_matrix_t* out, int out_map) -> Problem& {
     Problem& p = a.p[a.n_problems++];
@@ -883,9 +937,9 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
       Problem& p = add(d_ff, w, outs[i], 14 + i);
       p.segments = 1, p.depth = T, p.k_iters = t.stages(T), p.a_mn = 1;
       p.a_map[0] = p.a_map[1] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = p.b_map[1][0] = p.b_map[1][1] = 4;
-      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.depth, t.rows / 2);
+      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, a.mn_steps, t.rows / 2);
     }
-    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), t.depth, t.nh);
+    ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), a.mn_steps, t.nh);
   };
   auto add_x = [&]() {
     Problem& p = add(rows, x_class, dx, 16);
@@ -893,8 +947,8 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
     for (int i = 0; i < 2; ++i) {
       const nsp_matrix_t* weight = i ? w_up : w_gate;
       p.a_map[i] = 6 + 2 * i, p.b_map[i][0] = p.b_map[i][1] = 10 + 2 * i;
-      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, t.rows / 2, t.depth) &&
-           encode_operand(&maps.m[10 + 2 * i], weight->data, d_model, d_ff, ld_of(weight, d_ff, d_model), t.depth, t.nh);
+      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, a.a_rows, t.depth) &&
+           encode_operand(&maps.m[10 + 2 * i], weight->data, d_model, d_ff, ld_of(weight, d_ff, d_model), a.mn_steps, t.nh);
     }
   };
   const bool x_long = x_class.tiles > 0 && (w.tiles == 0 || x_class.per_split > w.per_split);

@@ -71,7 +71,7 @@ class Guarded:
             assert bool((whole == 7.0).all())
 
 
-SIZES = [(1, 8, 8), (1, 64, 128), (2, 72, 136), (77, 1024, 2816), (127, 128, 256), (128, 64, 128), (129, 520, 264), (255, 200, 1032),
+SIZES = [(1, 8, 8), (5, 128, 14336), (100, 264, 4000), (130, 392, 9480), (17, 2048, 264), (700, 128, 8200), (1, 64, 128), (2, 72, 136), (77, 1024, 2816), (127, 128, 256), (128, 64, 128), (129, 520, 264), (255, 200, 1032),
          (256, 256, 256), (257, 72, 136), (300, 2056, 520), (1000, 512, 1544), (513, 136, 8), (40, 8, 4096), (3, 4104, 24), (2500, 768, 2304),
          (4096, 136, 4736), (6001, 520, 3000), (9000, 136, 1160), (2560, 2568, 2056)]  # the last ones on tiles of 512 rows, one way or both
 
