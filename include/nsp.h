@@ -360,7 +360,7 @@ int nsp_rope(const nsp_rope_tensor_t* tensors, int32_t n_tensors, int32_t head_d
  *             dweight = sum over the rows of dy h, dbias = sum of dy
  * x, y, dy, dx are rows [outer, inner, dim] of dtype with element strides (0 .. 2^31) of the outer two axes (rows of a matrix:
  * inner = 1); weight, bias [dim] of w_dtype, NULL = 1 and 0; mean, rstd fp32 [outer * inner], written by the forward pass where
- * they are not NULL and read by the backward pass (RMS: mean is not read). dweight, dbias fp32 [dim], overwritten, either may be
+ * they are not NULL and read by the backward pass (RMS: mean is neither written nor read). dweight, dbias fp32 [dim], overwritten, either may be
  * NULL (not wanted). All sums are in fp32; dweight and dbias are added up in a fixed order (the same bits in every run). y may be
  * x, and dx may be x or dy, with the same strides; otherwise outputs overlap nothing. Rows of outputs must not overlap. Addresses
  * and strides that are multiples of 16 bytes and dim a multiple of 8 are fastest; any that fit the types will do.
@@ -452,6 +452,9 @@ int nsp_checked_withhold_load(nsp_plan_t* plan, int enable);
 /* The same for the backward kernel that runs on pairs of thread blocks: later backward launches leave out one tile load of the
  * second block, a tile of V or one of the fourth step (load = 0: none). UNSUPPORTED if the plan has no such items. */
 int nsp_checked_withhold_pair_load(nsp_plan_t* plan, int load);
+/* nsp_checked_withhold_glu_load(1 or 2): in later nsp_glu launches of the process the second CTA of the pair that has tile 0 leaves out
+ * its A or B tile of the second stage, and waits give up after two million SM clocks; 0: nothing is withheld. */
+int nsp_checked_withhold_glu_load(int load);
 #endif
 
 /* Kernels of the path, for nsp_plan_kernel_ms. */

@@ -44,7 +44,7 @@ EXPORTS = [
     "nsp_rope_frequencies", "nsp_rope", "nsp_norm_fwd", "nsp_norm_bwd_ws_bytes", "nsp_norm_bwd",
     "nsp_glu_fwd", "nsp_glu_bwd_ws_bytes", "nsp_glu_bwd", "nsp_glu_status",
 ]
-CHECKED_EXPORTS = ["nsp_checked_withhold_load", "nsp_checked_withhold_pair_load"]  # libnsp_checked.so only
+CHECKED_EXPORTS = ["nsp_checked_withhold_load", "nsp_checked_withhold_pair_load", "nsp_checked_withhold_glu_load"]  # libnsp_checked.so only
 NSP_COST_BUCKETS = 16
 NSP_STATIC_WS_BYTES = 32 * 1024 * 1024
 KERNEL_FWD, KERNEL_BWD_PRE, KERNEL_BWD_MAIN, KERNEL_BWD_POST, KERNEL_BWD_FIRST, KERNEL_FWD_FIRST = 0, 1, 2, 3, 4, 5
@@ -161,6 +161,8 @@ def lib() -> ctypes.CDLL:
             L.nsp_checked_withhold_load.restype = ctypes.c_int
             L.nsp_checked_withhold_pair_load.argtypes = [vp, ctypes.c_int]
             L.nsp_checked_withhold_pair_load.restype = ctypes.c_int
+            L.nsp_checked_withhold_glu_load.argtypes = [ctypes.c_int]
+            L.nsp_checked_withhold_glu_load.restype = ctypes.c_int
         L.nsp_selftest_wait_timeout.argtypes = [vp, ctypes.c_int64, vp]
         L.nsp_selftest_wait_timeout.restype = ctypes.c_int
         L.nsp_device_status.argtypes = [vp, i32p]
@@ -576,6 +578,15 @@ def nsp_checked_withhold_pair_load(plan: Plan, load: int):
     rc = lib().nsp_checked_withhold_pair_load(plan.handle, int(load))
     if rc != NSP_OK:
         raise NspError(rc, "nsp_checked_withhold_pair_load")
+
+
+def nsp_checked_withhold_glu_load(load: int):
+    """Checked build only: later nsp_glu launches leave out one tile load (1: of A, 2: of B, 0: none)."""
+    if not hasattr(lib(), "nsp_checked_withhold_glu_load"):
+        raise NspError(NSP_ERR_UNSUPPORTED, "nsp_checked_withhold_glu_load (needs libnsp_checked.so)")
+    rc = lib().nsp_checked_withhold_glu_load(int(load))
+    if rc != NSP_OK:
+        raise NspError(rc, "nsp_checked_withhold_glu_load")
 
 
 def nsp_device_status(plan: Plan):

@@ -18,6 +18,7 @@
 // A stage of an operand is one instruction of one warp: a 3-D box is several blocks of 64 columns at once. With stages of 64 steps
 // and boxes of 64 columns the kernel was bound by the number of TMA instructions a thread issues (16,384 tokens, 4,096 x 12,288: 2,700
 // us there and 7,000 back; boxes of 128 columns 2,670 and 5,790; stages of 128 steps 2,390 and 4,840).
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -44,7 +45,6 @@ static_assert(Geometry<false>::kStages * (Geometry<false>::kBytesA + Geometry<fa
 constexpr uint32_t kBlock = 128 * 64 * 2;  // bytes of a block of 128 rows x 64 columns
 constexpr int kThreads = 384;              // producer of A, issuer, producer of B, an idle warp, two warpgroups of epilogue
 constexpr int kGroupM = 8, kGroupTall = 4; // row tiles that are walked together (see tile_at)
-constexpr long long kWaitLimit = NSP_WAIT_CYCLES_DEFAULT;
 constexpr int kMostMaps = 20, kMostProblems = 3;
 
 struct Problem {
@@ -90,6 +90,10 @@ struct GemmArgs {
   int32_t a_rows, mn_steps, bytes_a, bytes_b, stages;
   Schedule order;
   StatusWord status;
+  // SM clocks a wait for operands may take before it gives up; the waits for another role's work may take twice that, so that the
+  // record names the load and not what stands behind it
+  long long wait_limit;
+  int32_t withhold;      // checked build only: the load the second CTA leaves out (1: A, 2: B; failure-detection test), or 0
   float* partial;  // [partial tile][CTA][4 columns][128 rows][4]: accumulators of tiles whose contraction is split
 };
 
@@ -310,7 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         const CUtensorMap* const map1 = &maps.m[is_a ? p.a_map[1] : p.b_map[1][mine]];  // of the second segment
         const Part part(p, tile - p.first_tile);
         for (int k = part.first; k < part.last; ++k, turn.next(stages)) {
-          if (*abort_flag || !mbar_wait(&s.empty[turn.st], turn.ph ^ 1, kWaitLimit)) {
+          if (*abort_flag || !mbar_wait(&s.empty[turn.st], turn.ph ^ 1, 2 * a.wait_limit)) {
             if (!*abort_flag) report_timeout(a.status, tile, kWhereGluEmpty, k);
             raise_abort();
             ok = false;
@@ -321,7 +325,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
           if (is_a && rank == 0)
             mbar_expect_tx(&s.full[turn.st], of_a * operand_bytes<kDepth>(p.a_mn, wide_a, a.mn_steps, at, p.depth) +
                                                  of_b * operand_bytes<kDepth>(p.b_mn, nh, a.mn_steps, at, p.depth));
-          if (across < end)
+          bool loads = across < end;
+#ifdef NSP_CHECKED
+          if (a.withhold == (is_a ? 1 : 2) && rank == 1 && tile == 0 && k == part.first + 1) loads = false;  // never arrives
+#endif
+          if (loads)
             load_operand<kDepth>(is_a ? stage_a(turn.st) : stage_b(turn.st), second ? map1 : map0, lead + off(&s.full[turn.st]), mn, across, at,
                                  wide, a.mn_steps, end, p.depth);
         }
@@ -347,7 +355,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       const Part part(p, tile - p.first_tile);
       const int iters = part.last - part.first;
       auto acc_free = [&](uint32_t which) -> bool {
-        const bool here = cluster_wait_tmem(&s.acc_empty[which], turn ^ 1, kWaitLimit);
+        const bool here = cluster_wait_tmem(&s.acc_empty[which], turn ^ 1, 2 * a.wait_limit);
         if (!__all_sync(0xffffffffu, here)) {
           if (lane == 0) report_timeout(a.status, tile, kWhereGluAccEmpty, static_cast<int32_t>(which)), raise_abort();
           return false;
@@ -356,7 +364,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
         return true;
       };
       auto arrived = [&](int k, const Turn& at) -> bool {
-        const bool here = *abort_flag == 0 && cluster_wait(&s.full[at.st], at.ph, kWaitLimit);
+        const bool here = *abort_flag == 0 && cluster_wait(&s.full[at.st], at.ph, a.wait_limit);
         if (!__all_sync(0xffffffffu, here)) {
           if (lane == 0 && !*abort_flag) report_timeout(a.status, tile, kWhereGluFull, k);
           if (lane == 0) raise_abort();
@@ -412,7 +420,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) glu_gem
       int m, n;
       tile_at<kGroup>(p, tile - p.first_tile, m, n);
       const uint32_t buf0 = kTall ? 0 : n_done & 1, turn = kTall ? n_done & 1 : (n_done >> 1) & 1;
-      const bool here = *abort_flag == 0 && mbar_wait(&s.acc_full[buf0], turn, kWaitLimit);
+      const bool here = *abort_flag == 0 && mbar_wait(&s.acc_full[buf0], turn, 2 * a.wait_limit);
       const int thread = quad * 32 + lane;
       const BlockOut out{s.out[half], half, thread};
       if (!out.all(here)) {  // the warpgroup goes on together: it meets at barriers below
@@ -613,6 +621,18 @@ struct DeviceRecord {
 constexpr int kMostDevices = 64;
 DeviceRecord g_records[kMostDevices];
 std::mutex g_mutex;
+
+#ifdef NSP_CHECKED
+std::atomic<int> g_withhold{0};
+#endif
+// How long a wait may take: the library's default, or where a load is withheld a thousandth of it.
+void set_waits(GemmArgs& a) {
+  a.wait_limit = NSP_WAIT_CYCLES_DEFAULT;
+#ifdef NSP_CHECKED
+  a.withhold = g_withhold.load();
+  if (a.withhold) a.wait_limit = 2000000;
+#endif
+}
 
 int record_of(DeviceRecord** out) {
   int dev = 0;
@@ -823,6 +843,7 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
   a.n_problems = 1;
   a.order = t.order;
   a.status = rec->word;
+  set_waits(a);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return (act == NSP_ACT_SILU ? launch_gemm<kSilu>(maps, a, t.tall, t.pairs, st) : launch_gemm<kGelu>(maps, a, t.tall, t.pairs, st)) == cudaSuccess
              ? NSP_OK : NSP_ERR_CUDA;
@@ -959,6 +980,7 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + activation_bytes(rows, d_ff));
   if (!ok) return NSP_ERR_CUDA;
   a.status = rec->word;
+  set_waits(a);
   count_launches(1);
   const int blocks = act_args.total / 256 + 1 < 148u * 8 ? static_cast<int>(act_args.total / 256 + 1) : 148 * 8;
   if (launch_chained_if(true, act == NSP_ACT_SILU ? glu_act_kernel<kSilu> : glu_act_kernel<kGelu>, blocks, 256, 0, st, act_args) != cudaSuccess)
@@ -986,3 +1008,11 @@ extern "C" int nsp_glu_status(int32_t out[4]) {
   for (int i = 0; i < 4; ++i) out[i] = reinterpret_cast<volatile int32_t*>(rec->host)[i];
   return NSP_OK;
 }
+
+#ifdef NSP_CHECKED
+extern "C" int nsp_checked_withhold_glu_load(int load) {
+  if (load < 0 || load > 2) return NSP_ERR_INVALID_ARG;
+  g_withhold.store(load);
+  return NSP_OK;
+}
+#endif

@@ -6,7 +6,9 @@ heads per GPU) and every length class b (segments of about 2^(b+5.5) tokens), an
 ``tcomp_ns[l][b]`` = nanoseconds per causal (query, key) pair and local query head, forward + backward: the profiled
 compute throughput the paper's cost model takes as an input (Sec. 4.1.2, SP-backend level). Length classes whose batch
 would exceed ``--max-pflop`` are not run; they take the value of the longest class that was (the time per pair no
-longer changes there). Needs a CUDA device.
+longer changes there). ``token_ops_ns`` is the library's part of the model's other term, the non-attention time of a layer per
+resident token (``other_ns_per_token`` of ``route_batch``): two norms of the hidden state, the rotation of queries and keys and the
+gated feed-forward block, forward and backward; a caller adds its own projections. Needs a CUDA device.
 """
 from __future__ import annotations
 
@@ -73,6 +75,53 @@ def measure(hq=32, hkv=4, n_levels=4, tokens=131072, max_pflop=1.5, iters=3, dev
     return table, rows
 
 
+def measure_token_ops(d_model, d_ff, hq=32, hkv=4, head_dim=128, tokens=16384, iters=3, device="cuda:0"):
+    """Nanoseconds per token, forward + backward, of what a layer does token by token in this library (dict by operator)."""
+    import torch
+
+    from .api import Rotary
+
+    dev, bf = torch.device(device), torch.bfloat16
+    g = torch.Generator(device=dev)
+    g.manual_seed(0)
+    rnd = lambda *shape: torch.randn(shape, device=dev, generator=g, dtype=torch.float32).to(bf)
+    new = lambda *shape, dtype=bf: torch.empty(shape, device=dev, dtype=dtype)
+    f32 = torch.float32
+    x, dy, y = rnd(tokens, d_model), rnd(tokens, d_model), new(tokens, d_model)
+    weight, rstd, dweight = torch.ones(d_model, device=dev), new(tokens, dtype=f32), new(d_model, dtype=f32)
+    q, k, rope = rnd(tokens, hq, head_dim), rnd(tokens, hkv, head_dim), Rotary(head_dim)
+    w_gate, w_up = rnd(d_ff, d_model), rnd(d_ff, d_model)
+    h, gate, up, dw_gate, dw_up = new(tokens, d_ff), new(tokens, d_ff), new(tokens, d_ff), new(d_ff, d_model), new(d_ff, d_model)
+    need = max(B.nsp_norm_bwd_ws_bytes(tokens, d_model), B.nsp_glu_bwd_ws_bytes(tokens, d_model, d_ff))
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+
+    def norm():
+        B.nsp_norm_fwd(x, weight, None, y, None, rstd, kind=B.NSP_NORM_RMS)
+        B.nsp_norm_bwd(x, dy, weight, None, rstd, y, dweight, None, ws, kind=B.NSP_NORM_RMS)
+
+    def rotation():
+        rope.rotate([q, k], [q, k], None)
+        rope.rotate([q, k], [q, k], None, inverse=True)
+
+    def glu():
+        B.nsp_glu_fwd(x, w_gate, w_up, h, gate, up)
+        B.nsp_glu_bwd(h, x, w_gate, w_up, gate, up, y, dw_gate, dw_up, ws)
+
+    out = {}
+    for name, step, times in (("norm", norm, 2), ("rotation", rotation, 1), ("feed_forward", glu, 1)):
+        step()
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(iters):
+            step()
+        e1.record()
+        torch.cuda.synchronize()
+        out[name] = times * e0.elapsed_time(e1) / iters * 1e6 / tokens
+    assert B.nsp_glu_status()[0] == 0
+    return out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--out", required=True)
@@ -80,6 +129,8 @@ def main():
     ap.add_argument("--hkv", type=int, default=4)
     ap.add_argument("--levels", type=int, default=4)
     ap.add_argument("--max-pflop", type=float, default=1.5)
+    ap.add_argument("--d-model", type=int, default=0, help="with --d-ff: measure the token-wise operators of a layer too")
+    ap.add_argument("--d-ff", type=int, default=0)
     args = ap.parse_args()
     import torch
 
@@ -88,10 +139,15 @@ def main():
            "written_by": "python -m paper_2609_22755_b200.measure_cost_table",
            "device": torch.cuda.get_device_name(0), "model": {"hq": args.hq, "hkv": args.hkv, "head_dim": 128},
            "levels": args.levels, "buckets": B.NSP_COST_BUCKETS, "tcomp_ns": table.tolist(), "runs": rows}
+    if args.d_model and args.d_ff:
+        ops = measure_token_ops(args.d_model, args.d_ff, args.hq, args.hkv)
+        doc["token_ops_ns"] = {**ops, "sum": sum(ops.values()), "d_model": args.d_model, "d_ff": args.d_ff}
     with open(args.out, "w") as f:
         json.dump(doc, f, indent=1)
     for r in rows:
         print(r)
+    if "token_ops_ns" in doc:
+        print(doc["token_ops_ns"])
 
 
 if __name__ == "__main__":

@@ -48,7 +48,8 @@ def route_batch(lengths, n_levels, b_tok, prefix_k=8, beam_w=4, monotone=True, h
     """Cost table -> Algorithm 1 -> per-GPU shards, through the library's host functions.
 
     link_gbs: bandwidth per level (default: 770 GB/s, the measured NVLink 5 peer copy, at every level above 0);
-    other_ns_per_token: non-attention time of one layer per resident token. Returns a dict with the routing
+    other_ns_per_token: non-attention time of one layer per resident token (``measure_cost_table`` times what this library has of
+    it: norms, rotation, gated feed-forward block). Returns a dict with the routing
     (level, index, load, tok, feasible), the cost table and the shards."""
     from . import binding as B
 

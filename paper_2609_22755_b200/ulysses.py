@@ -9,6 +9,10 @@ directly where the attention kernels read it: the block a peer s sends for sampl
 a token-major tensor is strided): ``nsp_a2a_gather_heads`` before the exchange, ``nsp_a2a_scatter_heads`` after the
 reverse exchange (which also adds the partial dK / dV of a KV head that several GPUs of the node share).
 
+Rotary positions are applied on the token slices, where every KV head is there once (behind the exchange a head that several GPUs
+share would be rotated by each of them): ``rope`` of the prologue rotates on the way in, of the epilogue the gradients on the way
+back; ``NodeLayout.positions`` are those of a GPU's slices.
+
 The layout steps run in the library's CUDA kernels (``CudaLayoutOps``); the exchange goes through
 ``torch.distributed`` (NCCL between GPUs). ``phase_streams`` runs the communication of the next node on its own stream
 while the current node computes (the paper's inter-level phase streaming in its simplest, two-queue form).
@@ -39,6 +43,9 @@ class CudaLayoutOps:
 
         B.nsp_a2a_gather_heads_to(src, dst_tensors, dst_row, sample_off, tokens, heads, heads_per_block, head_dim,
                                   first_head, stream)
+
+    def rotate(self, rope, x, y, positions, inverse, stream=None):
+        rope.rotate(x, y, positions, inverse=inverse, stream=stream)
 
 
 @dataclass
@@ -77,6 +84,13 @@ class NodeLayout:
         """(heads of the whole tensor, heads per peer, first head per peer) for 'q' or 'kv' shaped tensors."""
         return (self.hq, self.hq_loc, self.q_first) if kind == "q" else (self.hkv, self.hkv_loc, self.kv_first)
 
+    def positions(self, device=None):
+        """Positions of this GPU's tokens in their samples, int64 [t_loc]: slice r of a sample of L tokens begins at r L / d."""
+        import torch
+
+        parts = [torch.arange(self.rank * n, (self.rank + 1) * n) for n in self.tok_loc]
+        return torch.cat(parts or [torch.empty(0, dtype=torch.int64)]).to(device)
+
     def workload_segments(self):
         """Lengths and local head counts of this node's segments in the attention layout."""
         return [int(L) for L in self.lengths], self.hq_loc, self.hkv_loc
@@ -92,6 +106,17 @@ class UlyssesExchange:
             raise ValueError("group_ranks must list one global rank per GPU of the node")
         self.ops = ops if ops is not None else CudaLayoutOps()
         self.group = group
+        self._positions = {}
+
+    def _rotated(self, rope, x, inverse, stream, out=None):
+        """x [t_loc, H, D] rotated by the positions of its tokens, into out or a tensor of its own."""
+        import torch
+
+        if x.device not in self._positions:
+            self._positions[x.device] = self.lay.positions(x.device)
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        self.ops.rotate(rope, x, out, self._positions[x.device], inverse, stream)
+        return out
 
     def _exchange(self, send_of, recv_of):
         """One grouped exchange: send_of(peer, sample) / recv_of(peer, sample) return contiguous tensors."""
@@ -112,15 +137,18 @@ class UlyssesExchange:
             for req in dist.batch_isend_irecv(ops):
                 req.wait()
 
-    def to_attention_layout(self, x_loc, kind, out=None, stream=None):
+    def to_attention_layout(self, x_loc, kind, out=None, stream=None, rope=None):
         """x_loc [t_loc, H, D] (this GPU's token slices, all heads) -> [t_full, H / d, D]: complete sequences of the
-        node's samples, this GPU's heads, packed sample after sample (what nsp_attn_fwd / nsp_attn_bwd read)."""
+        node's samples, this GPU's heads, packed sample after sample (what nsp_attn_fwd / nsp_attn_bwd read). rope: a Rotary,
+        queries and keys are rotated by their positions first."""
         import torch
 
         lay = self.lay
         H, h_loc, first = lay.heads(kind)
         D = lay.head_dim
         x_loc = x_loc.reshape(lay.t_loc, H, D)
+        if rope is not None:
+            x_loc = self._rotated(rope, x_loc, False, stream)
         send = torch.empty((lay.degree, lay.t_loc, h_loc, D), dtype=x_loc.dtype, device=x_loc.device)
         self.ops.gather(x_loc, send, lay.t_loc, H, h_loc, D, first, stream)
         if out is None:
@@ -137,13 +165,13 @@ class UlyssesExchange:
         self._exchange(send_of, recv_of)
         return out
 
-    def store_to_attention_layouts(self, x_loc, kind, peer_buffers, stream=None):
+    def store_to_attention_layouts(self, x_loc, kind, peer_buffers, stream=None, rope=None):
         """The prologue without a staging buffer and without a separate exchange: this GPU's token slices go, head block
         by head block, straight into the packed attention buffers of the node's GPUs. peer_buffers[p] is GPU p's
         [t_full, H / d, D] buffer as a tensor this process can write (its own for p == rank; a peer's memory mapped
         into this process otherwise, e.g. through CUDA IPC or a symmetric-memory allocation). One kernel of the library
         issues plain stores; the caller orders it against the readers (every GPU of the node runs this call, then the
-        group synchronises, then attention runs)."""
+        group synchronises, then attention runs). rope: as for to_attention_layout."""
         import torch
 
         lay = self.lay
@@ -152,15 +180,18 @@ class UlyssesExchange:
         x_loc = x_loc.reshape(lay.t_loc, H, D)
         if len(peer_buffers) != lay.degree:
             raise ValueError("one attention buffer per GPU of the node")
+        if rope is not None:
+            x_loc = self._rotated(rope, x_loc, False, stream)
         # this GPU holds the token range [rank L_j / d, (rank + 1) L_j / d) of sample j, for every receiver alike
         rows = [[int(lay.full_off[j]) + lay.rank * lay.tok_loc[j] for j in range(len(lay.lengths))]] * lay.degree
         dst_row = torch.tensor(rows, dtype=torch.int64, device=x_loc.device)
         sample_off = torch.as_tensor(lay.loc_off, dtype=torch.int64).to(x_loc.device)
         self.ops.gather_to(x_loc, list(peer_buffers), dst_row, sample_off, lay.t_loc, H, h_loc, D, first, stream)
 
-    def from_attention_layout(self, y_full, kind, out=None, stream=None):
+    def from_attention_layout(self, y_full, kind, out=None, stream=None, rope=None):
         """The reverse: y_full [t_full, H / d, D] -> [t_loc, H, D]. Blocks that carry the same head (partial dK / dV of
-        a KV head shared by several GPUs) are added in fp32."""
+        a KV head shared by several GPUs) are added in fp32. rope: y_full is the gradient of rotated queries or keys, the result
+        that of the unrotated ones."""
         import torch
 
         lay = self.lay
@@ -181,6 +212,8 @@ class UlyssesExchange:
             out = torch.empty((lay.t_loc, H, D), dtype=y_full.dtype, device=y_full.device)
         out = out.reshape(lay.t_loc, H, D)
         self.ops.scatter(recv, out, lay.t_loc, H, h_loc, D, first, stream)
+        if rope is not None:
+            self._rotated(rope, out, True, stream, out)
         return out
 
 
