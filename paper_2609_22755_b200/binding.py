@@ -632,8 +632,26 @@ def nsp_attn_bwd_static(plan: Plan, q, k, v, o, d_o, lse, dq, dk, dv, softmax_sc
 
 # ---- token-wise operators around the attention
 # The small calls of these last about as long as the checks around them: structures are packed at once (struct) instead of field by
-# field, and every attribute of a tensor is asked for once.
+# field, every attribute of a tensor is asked for once, and what is needed of torch is looked up once (an import statement inside a
+# function costs 0.2 us each time).
 _ROPE_TENSOR, _ROWS, _MATRIX = (struct.Struct(f) for f in ("=QQQqqqqqii", "=Qqq", "=Qq"))
+
+
+class _Torch:
+    """Filled at the first call (the host-only functions of this module need no torch)."""
+
+    ready = False
+
+    @classmethod
+    def fill(cls):
+        import torch
+
+        cls.bf16, cls.f32, cls.i64 = torch.bfloat16, torch.float32, torch.int64
+        cls.Tensor, cls.current_device = torch.Tensor, torch.cuda.current_device
+        cls.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        cls.code = {torch.bfloat16: NSP_BF16, torch.float32: NSP_F32}
+        cls.both, cls.only_f32 = (torch.float32, torch.bfloat16), (torch.float32,)
+        cls.ready = True
 
 
 def _refuse(what, why, code=NSP_ERR_INVALID_ARG):
@@ -642,43 +660,36 @@ def _refuse(what, why, code=NSP_ERR_INVALID_ARG):
 
 def _on_device(what, names, tensors):
     """The current device; refuses tensors that are not on it (None is left out)."""
-    import torch
-
+    if not _Torch.ready:
+        _Torch.fill()
     here = None
     for t in tensors:
         if t is None:
             continue
-        at = t.get_device() if isinstance(t, torch.Tensor) else -1
-        if at < 0:
-            name = names[[x is t for x in tensors].index(True) % len(names)]
-            _refuse(what, f"{name} must be a CUDA tensor")
-        if here is None:
-            here = torch.cuda.current_device()
+        at = t.get_device() if isinstance(t, _Torch.Tensor) else -1
         if at != here:
             name = names[[x is t for x in tensors].index(True) % len(names)]
-            _refuse(what, f"{name} is on {t.device}, not on the current device")
+            if at < 0:
+                _refuse(what, f"{name} must be a CUDA tensor")
+            current = _Torch.current_device()
+            if at != current:
+                _refuse(what, f"{name} is on {t.device}, not on the current device")
+            here = current
     return here
 
 
 def _stream_on(here, stream):
     """As _stream_ptr, with the current device known."""
-    if stream is None and here is not None:
-        import torch
-
-        direct = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if direct:
-            return direct(here)
+    if stream is None and here is not None and _Torch.raw_stream:
+        return _Torch.raw_stream(here)
     return _stream_ptr(stream)
 
 
 def _dtype_of(what, name, dtype):
-    import torch
-
-    if dtype == torch.bfloat16:
-        return NSP_BF16
-    if dtype == torch.float32:
-        return NSP_F32
-    _refuse(what, f"{name} has dtype {dtype}")
+    code = _Torch.code.get(dtype)
+    if code is None:
+        _refuse(what, f"{name} has dtype {dtype}")
+    return code
 
 
 def nsp_rope_frequencies(rot_dim, base=10000.0, kind=NSP_ROPE_PLAIN, scale=1.0, trained_tokens=0.0, fast_turns=32.0,
@@ -698,10 +709,10 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
     """Rotate the heads of xs (a tensor [tokens, heads, head_dim], or a list of them with one head_dim) by their positions into
     ys (of the same shapes and types; x itself: in place), all in one launch. positions: int64 CUDA tensor [tokens], a list of
     them, or None (0, 1, 2, ...). inv_freq: float64 [rot_dim / 2] on the host. inverse: the gradient's way back."""
-    import torch
-
     what = "nsp_rope"
-    if isinstance(xs, torch.Tensor):
+    if not _Torch.ready:
+        _Torch.fill()
+    if isinstance(xs, _Torch.Tensor):
         xs, ys = [xs], [ys]
     if not isinstance(positions, (list, tuple)):
         positions = [positions] * len(xs)
@@ -715,7 +726,7 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
     if not xs:
         return
     here = _on_device(what, ("x", "y", "positions"), [t for group in zip(xs, ys, positions) for t in group])
-    packed, head_dim = [], xs[0].shape[-1]
+    packed, head_dim, known = [], xs[0].shape[-1], None
     for x, y, pos in zip(xs, ys, positions):
         shape, dtype, sx, sy = x.shape, x.dtype, x.stride(), y.stride()
         if len(shape) != 3 or shape[2] != head_dim or y.shape != shape or y.dtype != dtype:
@@ -723,12 +734,15 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
         if head_dim > 1 and (sx[2] != 1 or sy[2] != 1):
             _refuse(what, "the elements of a head must be contiguous")
         tokens, heads = shape[0], shape[1]
-        if pos is not None and (pos.dtype != torch.int64 or pos.shape != (tokens,) or not pos.is_contiguous()):
-            _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
+        if pos is None:
+            at = 0
+        elif pos is not known or tokens != known_tokens:
+            if pos.dtype != _Torch.i64 or pos.shape != (tokens,) or not pos.is_contiguous():
+                _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
+            known, known_tokens, at = pos, tokens, pos.data_ptr()
         if tokens * heads * head_dim == 0:
             continue
-        packed.append(_ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), 0 if pos is None else pos.data_ptr(), tokens, sx[0], sx[1], sy[0],
-                                        sy[1], heads, _dtype_of(what, "x", dtype)))
+        packed.append(_ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), at, tokens, sx[0], sx[1], sy[0], sy[1], heads, _dtype_of(what, "x", dtype)))
     rc = lib().nsp_rope(b"".join(packed), len(packed), head_dim, 2 * len(freq), int(layout), freq.tobytes(), float(magnitude),
                         1 if inverse else 0, _stream_on(here, stream))
     if rc != NSP_OK:
@@ -767,12 +781,10 @@ def _norm_vector(what, name, t, n, dtypes):
 def nsp_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NSP_NORM_LAYER, stream=None):
     """Layer norm or RMS norm of the rows of x [rows, dim] or [outer, inner, dim] into y (x itself: in place). weight, bias [dim]
     (bf16 or fp32, None = 1 and 0); mean, rstd: fp32, one entry per row, for the backward pass (None: not wanted)."""
-    import torch
-
-    what, both, f32 = "nsp_norm_fwd", (torch.float32, torch.bfloat16), (torch.float32,)
+    what = "nsp_norm_fwd"
     here = _on_device(what, ("x", "y", "weight", "bias", "mean", "rstd"), (x, y, weight, bias, mean, rstd))
     outer, inner, dim, dtype = _norm_shape(what, x)
-    rows = outer * inner
+    rows, both, f32 = outer * inner, _Torch.both, _Torch.only_f32
     rx, ry = _rows(what, "x", x, x.shape, x.dtype), _rows(what, "y", y, x.shape, x.dtype)
     w, b = _norm_vector(what, "weight", weight, dim, both), _norm_vector(what, "bias", bias, dim, both)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
@@ -781,7 +793,7 @@ def nsp_norm_fwd(x, weight, bias, y, mean, rstd, eps=1e-5, kind=NSP_NORM_LAYER, 
     if rows == 0 or dim == 0:
         return
     one = weight if weight is not None else bias
-    w_dtype = NSP_BF16 if one is not None and one.dtype == torch.bfloat16 else NSP_F32
+    w_dtype = NSP_BF16 if one is not None and one.dtype == _Torch.bf16 else NSP_F32
     rc = lib().nsp_norm_fwd(rx, w, b, ry, m, r, outer, inner, dim, dtype, w_dtype, int(kind), float(eps), _stream_on(here, stream))
     if rc != NSP_OK:
         raise NspError(rc, what)
@@ -799,13 +811,11 @@ def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NOR
     """Backward pass of nsp_norm_fwd: dx of x's shape and type (x or dy itself: in place), dweight and dbias fp32 [dim]
     (overwritten; None: not wanted). ws: a CUDA tensor of at least nsp_norm_bwd_ws_bytes(rows, dim) bytes (None where neither
     is wanted)."""
-    import torch
-
-    what, both, f32 = "nsp_norm_bwd", (torch.float32, torch.bfloat16), (torch.float32,)
+    what = "nsp_norm_bwd"
     here = _on_device(what, ("x", "dy", "dx", "weight", "mean", "rstd", "dweight", "dbias", "ws"),
                       (x, dy, dx, weight, mean, rstd, dweight, dbias, ws))
     outer, inner, dim, dtype = _norm_shape(what, x)
-    rows = outer * inner
+    rows, both, f32 = outer * inner, _Torch.both, _Torch.only_f32
     rx, rdy, rdx = (_rows(what, name, t, x.shape, x.dtype) for name, t in (("x", x), ("dy", dy), ("dx", dx)))
     w = _norm_vector(what, "weight", weight, dim, both)
     dw, db = _norm_vector(what, "dweight", dweight, dim, f32), _norm_vector(what, "dbias", dbias, dim, f32)
@@ -815,7 +825,7 @@ def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NOR
     _check_ws(what, ws)
     if dim == 0:
         return
-    w_dtype = NSP_BF16 if weight is not None and weight.dtype == torch.bfloat16 else NSP_F32
+    w_dtype = NSP_BF16 if weight is not None and weight.dtype == _Torch.bf16 else NSP_F32
     rc = lib().nsp_norm_bwd(rx, rdy, w, m, r, rdx, dw, db, outer if rows else 0, inner if rows else 1, dim, dtype, w_dtype, int(kind),
                             None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(),
                             _stream_on(here, stream))
@@ -825,11 +835,9 @@ def nsp_norm_bwd(x, dy, weight, mean, rstd, dx, dweight, dbias, ws, kind=NSP_NOR
 
 def _matrix(what, name, t, rows, cols):
     """A packed nsp_matrix_t of a bf16 tensor [rows, cols] with contiguous rows (None: a null pointer)."""
-    import torch
-
     if t is None:
         return None
-    if t.dtype != torch.bfloat16:
+    if t.dtype != _Torch.bf16:
         _refuse(what, f"{name} has dtype {t.dtype}")
     strides = t.stride()
     if t.shape != (rows, cols) or (cols > 1 and strides[1] != 1):

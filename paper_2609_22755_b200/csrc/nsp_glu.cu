@@ -675,12 +675,13 @@ bool encode_plain(CUtensorMap* out, const void* base, int64_t cols, int64_t rows
 }
 // The two maps of an operand (see load_operand): boxes of `box_rows` rows and several blocks of 64 columns, and the plain matrix.
 // The first one covers whole blocks alone, so that no box of it reads past the end of a row.
+// The plain one is left out where no box is cut.
 bool encode_operand(CUtensorMap* out, const void* base, int64_t cols, int64_t rows, int64_t ld, int box_rows, int box_cols) {
   const int blocks = box_cols / 64;
   const cuuint64_t dims[3] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols < 64 ? 1 : cols / 64)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, 128};
   const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(blocks)};
-  return encode(out, base, 3, dims, strides, box) && encode_plain(out + 1, base, cols, rows, ld, box_rows);
+  return (cols < box_cols || encode(out, base, 3, dims, strides, box)) && (cols % box_cols == 0 || encode_plain(out + 1, base, cols, rows, ld, box_rows));
 }
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
@@ -721,8 +722,14 @@ template <int kAct>
 cudaError_t launch_gemm(const Maps& maps, const GemmArgs& a, bool tall, int pairs, cudaStream_t st) {
   static_assert(sizeof(Maps) + sizeof(GemmArgs) <= 4000, "kernel parameters");
   void (*kernel)(const Maps, const GemmArgs) = tall ? glu_gemm_kernel<kAct, true> : glu_gemm_kernel<kAct, false>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Smem)));
-  if (e != cudaSuccess) return e;
+  static std::atomic<uint64_t> allowed[2];  // by device: the kernel may use that much shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && !(allowed[tall].load(std::memory_order_relaxed) >> dev & 1)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(Smem)));
+    if (e == cudaSuccess) allowed[tall].fetch_or(uint64_t{1} << dev, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return cudaGetLastError(), e;
   count_launches(1);
   return launch_chained_if(true, kernel, 2 * pairs, kThreads, sizeof(Smem), st, maps, a);
 }
@@ -834,7 +841,7 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
     if (!outs[i]) continue;
     p.out[i] = static_cast<__nv_bfloat16*>(const_cast<void*>(outs[i]->data));
     p.ld[i] = ld_of(outs[i], rows, d_ff);
-    if (!encode_plain(&maps.m[p.out_map + i], outs[i]->data, d_ff, rows, p.ld[i], 128)) return NSP_ERR_CUDA;
+    if (t.nh == 128 && !encode_plain(&maps.m[p.out_map + i], outs[i]->data, d_ff, rows, p.ld[i], 128)) return NSP_ERR_CUDA;
   }
   if (!encode_operand(&maps.m[0], x->data, d_model, rows, ld_of(x, rows, d_model), a.a_rows, t.depth) ||
       !encode_operand(&maps.m[2], w_gate->data, d_model, d_ff, ld_of(w_gate, d_ff, d_model), a.nh, t.depth) ||
@@ -947,7 +954,7 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
     p.rows = static_cast<int32_t>(out_rows), p.cols = d_model, p.b_mn = p.b_shared = 1;
     p.splits = c.splits, p.per_split = c.per_split, p.part = n_partial;
     p.out_map = out_map, p.out[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(out->data)), p.ld[0] = ld_of(out, out_rows, d_model);
-    ok = ok && encode_plain(&maps.m[out_map], out->data, d_model, out_rows, p.ld[0], 128);
+    if (c.splits == 1) ok = ok && encode_plain(&maps.m[out_map], out->data, d_model, out_rows, p.ld[0], 128);
     n_tiles += p.tiles_m * p.tiles_n * c.splits;
     if (c.splits > 1) n_partial += p.tiles_m * p.tiles_n * c.splits;
     return p;
