@@ -574,8 +574,8 @@ __global__ void __launch_bounds__(256) glu_sum_kernel(const __grid_constant__ Su
 // dg and du, 8 values a thread and access. HBM-bound: three reads and two writes of 2 bytes a value.
 struct ActArgs {
   const __nv_bfloat16 *g, *u, *dh;
-  __nv_bfloat16 *dg, *du;  // [rows, ff], contiguous
-  int64_t ld_g, ld_u, ld_dh;
+  __nv_bfloat16 *dg, *du;  // [rows, ff], rows on lines of 128 bytes
+  int64_t ld_g, ld_u, ld_dh, ld;
   uint32_t per_row, total;  // vectors
 };
 template <int kAct>
@@ -603,8 +603,8 @@ __global__ void __launch_bounds__(256) glu_act_kernel(const ActArgs a) {
       dg[k] = pack_bf16x2(o[0], o[1]);
       du[k] = pack_bf16x2(q[0], q[1]);
     }
-    reinterpret_cast<uint4*>(a.dg)[i] = make_uint4(dg[0], dg[1], dg[2], dg[3]);
-    reinterpret_cast<uint4*>(a.du)[i] = make_uint4(du[0], du[1], du[2], du[3]);
+    reinterpret_cast<uint4*>(a.dg + row * a.ld)[v] = make_uint4(dg[0], dg[1], dg[2], dg[3]);
+    reinterpret_cast<uint4*>(a.du + row * a.ld)[v] = make_uint4(du[0], du[1], du[2], du[3]);
   }
 }
 
@@ -857,7 +857,9 @@ extern "C" int nsp_glu_fwd(const nsp_matrix_t* x, const nsp_matrix_t* w_gate, co
 }
 
 namespace {
-size_t activation_bytes(int64_t rows, int32_t d_ff) { return (2 * 2 * static_cast<size_t>(rows) * d_ff + 255) / 256 * 256; }
+// dg and du in the workspace: rows that begin on lines of 128 bytes, so that a box of a TMA copy touches no more lines than it has
+int64_t activation_ld(int32_t d_ff) { return (d_ff + 63) / 64 * 64; }
+size_t activation_bytes(int64_t rows, int32_t d_ff) { return (2 * 2 * static_cast<size_t>(rows) * activation_ld(d_ff) + 255) / 256 * 256; }
 // Partial tiles of split contractions: no more than kMostPartial tiles of 256 x 256 fp32
 constexpr int kMostPartial = 96;
 constexpr size_t kPartialBytes = static_cast<size_t>(kMostPartial) * 256 * 256 * 4;
@@ -902,7 +904,7 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
   act_args.g = static_cast<const __nv_bfloat16*>(g->data), act_args.ld_g = ld_of(g, rows, d_ff);
   act_args.u = static_cast<const __nv_bfloat16*>(u->data), act_args.ld_u = ld_of(u, rows, d_ff);
   act_args.dh = static_cast<const __nv_bfloat16*>(dh->data), act_args.ld_dh = ld_of(dh, rows, d_ff);
-  act_args.dg = static_cast<__nv_bfloat16*>(ws), act_args.du = act_args.dg + rows * d_ff;
+  act_args.dg = static_cast<__nv_bfloat16*>(ws), act_args.ld = activation_ld(d_ff), act_args.du = act_args.dg + rows * act_args.ld;
   act_args.per_row = d_ff / 8, act_args.total = static_cast<uint32_t>(rows * (d_ff / 8));
   GemmArgs a = {};
   Maps maps;
@@ -965,7 +967,7 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
       Problem& p = add(d_ff, w, outs[i], 14 + i);
       p.segments = 1, p.depth = T, p.k_iters = t.stages(T), p.a_mn = 1;
       p.a_map[0] = p.a_map[1] = 2 * i, p.b_map[0][0] = p.b_map[0][1] = p.b_map[1][0] = p.b_map[1][1] = 4;
-      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, a.mn_steps, t.rows / 2);
+      ok = ok && encode_operand(&maps.m[2 * i], i ? act_args.du : act_args.dg, d_ff, rows, act_args.ld, a.mn_steps, t.rows / 2);
     }
     ok = ok && encode_operand(&maps.m[4], x->data, d_model, rows, ld_of(x, rows, d_model), a.mn_steps, t.nh);
   };
@@ -975,7 +977,7 @@ extern "C" int nsp_glu_bwd(const nsp_matrix_t* dh, const nsp_matrix_t* x, const 
     for (int i = 0; i < 2; ++i) {
       const nsp_matrix_t* weight = i ? w_up : w_gate;
       p.a_map[i] = 6 + 2 * i, p.b_map[i][0] = p.b_map[i][1] = 10 + 2 * i;
-      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, d_ff, a.a_rows, t.depth) &&
+      ok = ok && encode_operand(&maps.m[6 + 2 * i], i ? act_args.du : act_args.dg, d_ff, rows, act_args.ld, a.a_rows, t.depth) &&
            encode_operand(&maps.m[10 + 2 * i], weight->data, d_model, d_ff, ld_of(weight, d_ff, d_model), a.mn_steps, t.nh);
     }
   };
