@@ -115,13 +115,26 @@ static_assert(sizeof(Smem) <= 232448, "shared memory budget (227 KB)");
 
 enum Act : int32_t { kSilu = NSP_ACT_SILU, kGelu = NSP_ACT_GELU };
 
-// act(x), and its slope; exp and erfc are CUDA's. The normal distribution function is erfc(-x / sqrt 2) / 2: as (1 + erf) / 2 it
-// would have no correct digit left for x below -5.
-__device__ __forceinline__ float normal_cdf(float x) { return 0.5f * erfcf(x * -0.70710678118654752f); }
+// act(x), and its slope; exp is CUDA's. The normal distribution function at -t, t >= 0, is exp(-t^2 / 2) times a smooth function that falls
+// from 1/2 as 1 / t: s times a polynomial in s = 1 / (1 + 0.31 t), fitted for the smallest relative error by reweighted least squares
+// (1.7e-7; 4.7e-7 with the roundings of fp32, and t^2 / 2 ulp of the exponential). The slope needs the same exponential. (4,099 x 5,512
+// backward: 61 us with erfc and an exponential of its own, 40 so; 16,384 x 12,288 forward, in the epilogue: 2,256 and 2,220.)
+__device__ __forceinline__ float normal_cdf(float x, float bell) {  // bell: exp(-x^2 / 2)
+  const float s = __fdividef(1.f, fmaf(0.31f, fabsf(x), 1.f));
+  float q = fmaf(s, 0.0358906873f, -0.141819388f);
+  q = fmaf(q, s, 0.155459404f);
+  q = fmaf(q, s, -0.0152864568f);
+  q = fmaf(q, s, 0.110326536f);
+  q = fmaf(q, s, 0.107700795f);
+  q = fmaf(q, s, 0.124072447f);
+  q = fmaf(q, s, 0.123656064f);
+  const float tail = bell * s * q;
+  return x > 0.f ? 1.f - tail : tail;
+}
 template <int kAct>
 __device__ __forceinline__ float act_value(float x) {
   if constexpr (kAct == kSilu) return __fdividef(x, 1.f + __expf(-x));
-  return x * normal_cdf(x);
+  return x * normal_cdf(x, __expf(-0.5f * x * x));
 }
 template <int kAct>
 __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
@@ -130,9 +143,9 @@ __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
     value = x * p;
     slope = p * (1.f + x * (1.f - p));
   } else {
-    const float p = normal_cdf(x);
+    const float bell = __expf(-0.5f * x * x), p = normal_cdf(x, bell);
     value = x * p;
-    slope = fmaf(x * 0.39894228040143268f, __expf(-0.5f * x * x), p);
+    slope = fmaf(x * 0.39894228040143268f, bell, p);
   }
 }
 
