@@ -385,7 +385,7 @@ int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const void* weight, 
  * The gated half of a feed-forward block: both projections, the activation and the product, forward and backward.
  *   forward   g = x w_gate^T, u = x w_up^T, h = act(g) u
  *   backward  dg = dh u act'(g), du = dh act(g); dw_gate = dg^T x, dw_up = du^T x, dx = dg w_gate + du w_up
- * act: NSP_ACT_SILU (x / (1 + e^-x)) or NSP_ACT_GELU (x times the normal distribution function, by erf).
+ * act: NSP_ACT_SILU (x / (1 + e^-x)) or NSP_ACT_GELU (x times the normal distribution function).
  * x, dx [rows, d_model]; w_gate, w_up, dw_gate, dw_up [d_ff, d_model]; h, dh, g, u [rows, d_ff]: bf16 matrices with element
  * strides between rows (at least the row's length, multiples of 8) and 16-byte aligned addresses; d_model and d_ff multiples of 8.
  * The forward pass writes g and u for the backward pass where they are not NULL. Products accumulate in fp32; h is formed from
@@ -393,8 +393,8 @@ int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const void* weight, 
  * The gradients are overwritten; dx may be NULL (not wanted), and so may dw_gate and dw_up together. Outputs overlap nothing else.
  * ws: at least nsp_glu_bwd_ws_bytes(rows, d_model, d_ff), 256-byte aligned; contents undefined afterwards, and not shared by calls
  * that may overlap. The results are the same bits in every run.
- * Errors: INVALID_ARG, UNSUPPORTED (d_model or d_ff not a multiple of 8 or above NSP_GLU_MAX_DIM, rows * d_ff >= 2^34, a device
- * other than sm_100), WORKSPACE, CUDA, DEVICE_TIMEOUT.
+ * Errors: INVALID_ARG, UNSUPPORTED (d_model or d_ff not a multiple of 8 or above NSP_GLU_MAX_DIM, 2^30 or more rows, rows * d_ff >= 2^34,
+ * a device other than sm_100), WORKSPACE, CUDA, DEVICE_TIMEOUT.
  *
  * The kernels of these calls belong to no plan: a device-side wait that runs out (about two seconds) is recorded once per device,
  * every later nsp_glu call on it answers with DEVICE_TIMEOUT, and nsp_glu_status synchronises the current device and reads the

@@ -634,6 +634,7 @@ def nsp_attn_bwd_static(plan: Plan, q, k, v, o, d_o, lse, dq, dk, dv, softmax_sc
 # The small calls of these last about as long as the checks around them: structures are packed at once (struct) instead of field by
 # field, every attribute of a tensor is asked for once, and what is needed of torch is looked up once (an import statement inside a
 # function costs 0.2 us each time).
+_INT32_MAX = 2 ** 31 - 1
 _ROPE_TENSOR, _ROWS, _MATRIX = (struct.Struct(f) for f in ("=QQQqqqqqii", "=Qqq", "=Qq"))
 
 
@@ -734,6 +735,8 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
         if head_dim > 1 and (sx[2] != 1 or sy[2] != 1):
             _refuse(what, "the elements of a head must be contiguous")
         tokens, heads = shape[0], shape[1]
+        if heads > _INT32_MAX or head_dim > NSP_ROPE_MAX_HEAD_DIM:  # the library takes them in 32 bits
+            _refuse(what, f"x has shape {tuple(shape)}", NSP_ERR_UNSUPPORTED)
         if pos is None:
             at = 0
         elif pos is not known or tokens != known_tokens:
@@ -763,10 +766,14 @@ def _norm_shape(what, x):
     """(outer, inner, dim, dtype code) of x."""
     shape = x.shape
     if len(shape) == 2:
-        return shape[0], 1, shape[1], _dtype_of(what, "x", x.dtype)
-    if len(shape) == 3:
-        return shape[0], shape[1], shape[2], _dtype_of(what, "x", x.dtype)
-    _refuse(what, "x must be [rows, dim] or [outer, inner, dim]")
+        outer, inner, dim = shape[0], 1, shape[1]
+    elif len(shape) == 3:
+        outer, inner, dim = shape
+    else:
+        _refuse(what, "x must be [rows, dim] or [outer, inner, dim]")
+    if inner > _INT32_MAX or dim > NSP_NORM_MAX_DIM:  # the library takes them in 32 bits
+        _refuse(what, f"x has shape {tuple(shape)}", NSP_ERR_UNSUPPORTED)
+    return outer, inner, dim, _dtype_of(what, "x", x.dtype)
 
 
 def _norm_vector(what, name, t, n, dtypes):
@@ -849,6 +856,8 @@ def _glu_sizes(what, x, w_gate):
     sx, sw = x.shape, w_gate.shape
     if len(sx) != 2 or len(sw) != 2:
         _refuse(what, "x is [rows, d_model], w_gate and w_up are [d_ff, d_model]")
+    if sx[1] > NSP_GLU_MAX_DIM or sw[0] > NSP_GLU_MAX_DIM:  # the library takes them in 32 bits
+        _refuse(what, f"d_model {sx[1]}, d_ff {sw[0]}", NSP_ERR_UNSUPPORTED)
     return sx[0], sx[1], sw[0]
 
 

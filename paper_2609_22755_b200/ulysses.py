@@ -109,12 +109,17 @@ class UlyssesExchange:
         self._positions = {}
 
     def _rotated(self, rope, x, inverse, stream, out=None):
-        """x [t_loc, H, D] rotated by the positions of its tokens, into out or a tensor of its own."""
+        """x [t_loc, H, D] rotated by the positions of its tokens, into out or a tensor of its own (of that stream)."""
         import torch
 
         if x.device not in self._positions:
             self._positions[x.device] = self.lay.positions(x.device)
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        if out is None:
+            owner = stream
+            if isinstance(stream, int):
+                owner = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+            with torch.cuda.stream(owner):
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         self.ops.rotate(rope, x, out, self._positions[x.device], inverse, stream)
         return out
 

@@ -234,3 +234,27 @@ def test_cost_table_times_the_token_operators(B):
 
     ops = measure_token_ops(256, 512, 4, 2, tokens=512, iters=1)
     assert set(ops) == {"norm", "rotation", "feed_forward"} and all(v > 0 for v in ops.values())
+
+
+def test_node_layouts_with_rope_on_another_stream(B):
+    """The rotated copy belongs to the stream that the calls are given: what the current stream allocates meanwhile is other memory."""
+    import torch
+
+    from paper_2609_22755_b200.api import Rotary
+    from paper_2609_22755_b200.ulysses import NodeLayout, UlyssesExchange
+
+    lay, rope, side = NodeLayout([9600, 3300], 1, 0, 8, 2, 128), Rotary(128), torch.cuda.Stream()
+    ex = UlyssesExchange(lay, [0])
+    x = torch.randn(12900, 8, 128, device="cuda")
+    want = torch.empty_like(x)
+    rope.rotate(x, want, torch.cat([torch.arange(9600), torch.arange(3300)]).cuda())
+    for stream in (side, side.cuda_stream):
+        into = [torch.zeros_like(x)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(10_000_000)  # the calls below run behind this
+        ex.store_to_attention_layouts(x, "q", into, rope=rope, stream=stream)
+        others = [torch.full_like(x, 7.0) for _ in range(4)]
+        side.synchronize()
+        assert torch.equal(into[0], want)
+        del others

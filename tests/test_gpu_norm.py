@@ -252,3 +252,39 @@ def test_streams_and_graphs(B):
         graph.replay()
         step(want)
         assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("dim", [129, 300, 2051, 4104, 5511, 16383])
+def test_in_place_with_many_rows_to_a_block(B, dim, kind):
+    """Rows of 2,051 bf16 share their 16-byte pieces with neighbours that other blocks write."""
+    import torch
+
+    rows = 4000
+    x, dy = make((rows, dim), torch.bfloat16, 1), make((rows, dim), torch.bfloat16, 2)
+    w = torch.randn(dim, device="cuda")
+    y, mu, r = torch.empty_like(x), torch.empty(rows, device="cuda") if kind == 0 else None, torch.empty(rows, device="cuda")
+    B.nsp_norm_fwd(x, w, w, y, mu, r, kind=kind)
+    z = x.clone()
+    B.nsp_norm_fwd(z, w, w, z, None, None, kind=kind)
+    assert torch.equal(y, z)
+    ws = torch.empty(B.nsp_norm_bwd_ws_bytes(rows, dim), dtype=torch.uint8, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    B.nsp_norm_bwd(x, dy, w, mu, r, dx, dw, db, ws, kind=kind)
+    for onto_x in (True, False):
+        xx, gg, dw2, db2 = x.clone(), dy.clone(), torch.empty_like(dw), torch.empty_like(db)
+        into = xx if onto_x else gg
+        B.nsp_norm_bwd(xx, gg, w, mu, r, into, dw2, db2, ws, kind=kind)
+        assert torch.equal(into, dx) and torch.equal(dw2, dw) and torch.equal(db2, db)
+
+
+def test_sizes_beyond_32_bits_are_refused(B):
+    """A size that 32 bits cut to a small one must not become a call with that one."""
+    import torch
+
+    x = torch.zeros(1, 1, 8, device="cuda").expand(1, 2 ** 32 + 1, 8)
+    w = torch.ones(8, device="cuda")
+    for call in (lambda: B.nsp_norm_fwd(x, w, None, x, None, None), lambda: B.nsp_rope([x], [x], None, [0.5, 0.25]),
+                 lambda: B.nsp_norm_fwd(x[0], w, None, x[0], None, None)):
+        with pytest.raises(B.NspError):
+            call()
