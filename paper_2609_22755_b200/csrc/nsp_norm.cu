@@ -376,9 +376,10 @@ __device__ __forceinline__ void row_of(uint32_t r, int inner, int64_t& o, int& i
 
 // kLanes lanes (a warp: kWarps of them) a row, kVecs vectors a lane, kRows rows a team
 constexpr int fwd_threads(int warps) { return warps > 4 ? 32 * warps : 128; }
-// Blocks an SM the registers are cut to: five where four vectors a lane are under way (2,048: 50 -> 46 us for 32,768 rows), else the
-// compiler's choice (512: 50 us, cut 54).
-constexpr int fwd_blocks(int vecs, int warps) { return vecs != 4 ? 0 : warps <= 4 ? 5 : warps == 8 ? 2 : 1; }
+// Blocks an SM the registers are cut to: five where four vectors a lane are under way (2,048: 50 -> 46 us for 32,768 rows); two or three of
+// the longest rows, a row a block, so that some load while others store (4,096 x 16,384: 78 us with one block of two rows, 67 so); else
+// the compiler's choice (512: 50 us, cut 54).
+constexpr int fwd_blocks(int vecs, int warps) { return vecs == 8 && warps == 8 ? 3 : vecs != 4 ? 0 : warps <= 4 ? 5 : 2; }
 template <typename T, int kLanes, int kVecs, int kWarps, int kRows, bool kLayer>
 __global__ void __launch_bounds__(fwd_threads(kWarps), fwd_blocks(kVecs, kWarps)) norm_fwd_kernel(const NormArgs a) {
   constexpr int kTeam = kLanes * kWarps, kTeams = fwd_threads(kWarps) / kTeam;
@@ -659,7 +660,9 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
 
 // Long rows: several warps a row, kVecs vectors a thread, a.stages rows ahead. A block has one or more teams, which go on together (one
 // barrier a row). One row at a time: two at one barrier take more registers than two blocks an SM have (32,768 x 4,096: 141 us, with
-// two rows 276, and 512 threads of one vector 298).
+// two rows 276, and 512 threads of one vector 298). Rows of more than 8,192 elements take four vectors a thread: halves of a row in the CTAs
+// of a cluster, its barrier hidden behind the next row's sums, gain with two sums a row and lose with one (4,096 x 16,384: layer norm 143 us,
+// halves 123; RMS 110 and 111; 4,096 x 12,288 RMS 96 and 104; 8,192 x 8,320 193 and 205).
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, uint32_t bytes) {  // 16, or none: zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -1089,7 +1092,8 @@ Launch fwd_launch(int dim, int64_t rows) {
     if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 4, 2);
     else NSP_USE(32, 4, 8, 2);
   }
-  else NSP_USE(32, 4, 16, 2);
+  else if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 8, 1);
+  else NSP_USE(32, 4, 16, 1);
 #undef NSP_USE
   l.blocks = (rows + per_block - 1) / per_block;
   return l;
