@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
   const int team = static_cast<int>(threadIdx.x) / team_threads, tid = static_cast<int>(threadIdx.x) - team * team_threads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team_warps = team_threads >> 5;
   const int n_vec = team < teams ? a.dim / 8 : 0, stages = a.stages;
-  // Weights and the row stay in registers between the sums and dx; with four vectors a thread there is no room for them: the weights
+  // Weights and the row stay in registers between the sums and dx; with more than two vectors a thread there is no room for them: the weights
   // are loaded again, and the row is read again from its stage, which is then filled anew behind that.
   constexpr int kHeld = kVecs > 2 ? 0 : kVecs;
   using B = BwdVec<T, kKind>;
@@ -712,6 +712,9 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
       return w;
     }
   };
+  // With three vectors a thread, a warp leaves out those that none of its lanes has: a row of 8,320 elements takes little more than two (8,192
+  // rows: 156 us, with four vectors of 288 threads 193; 4,096 x 12,288 105 and 125). With four the branches cost more (4,096 x 16,384: 143 us, 153 with them).
+  auto idle = [&](int j) { return kVecs == 3 && (tid & ~31) + j * team_threads >= n_vec; };
   const uint32_t mine = smem_u32(ring) + threadIdx.x * kVecBytes;
   const int64_t step = static_cast<int64_t>(gridDim.x) * teams;
   const int64_t start = static_cast<int64_t>(blockIdx.x) * teams + team;
@@ -726,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
     const bool here = in.r < a.rows;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
+      if (idle(j)) continue;
       const uint32_t bytes = here && on[j] ? 16 : 0;
 #pragma unroll
       for (int e = 0; e < kVecBytes; e += 16) {
@@ -754,6 +758,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
     F2 s{0}, c{0};
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
+      if (idle(j)) continue;
       read(j);
       B::sums(x[j], dy[j], weights(j), both(r), both(shift), s, c, dw[j], db[j]);
     }
@@ -786,6 +791,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
     const bool here = out.r < a.rows;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
+      if (idle(j)) continue;
       if (!kHeld) read(j);
       B::grad(x[j], dy[j], weights(j), both(r), both(slope), both(offset), out.p[0], tid + j * team_threads, here && on[j]);
     }
@@ -1113,12 +1119,13 @@ Launch bwd_launch(int dim, int64_t rows) {
   else if (n <= 32) brief(norm_bwd_short_kernel<T, 16, 2, 2, kKind>, 16, 2);
   else if (n <= 64) brief(norm_bwd_short_kernel<T, 32, 2, 2, kKind>, 32, 2);
   else {
-    const int vecs = n > 1024 ? 4 : 2;
-    if (n > 1024) l.kernel = norm_bwd_long_kernel<T, 512, 4, kKind>;
+    const int vecs = n > 1536 ? 4 : n > 1024 ? 3 : 2;
+    if (n > 1536) l.kernel = norm_bwd_long_kernel<T, 512, 4, kKind>;
+    else if (n > 1024) l.kernel = norm_bwd_long_kernel<T, 512, 3, kKind>;
     else if (n > 512) l.kernel = norm_bwd_long_kernel<T, 512, 2, kKind>;
     else l.kernel = norm_bwd_long_kernel<T, 256, 2, kKind>;
     l.threads = n > 512 ? 512 : 256;
-    l.team = round32((n + vecs - 1) / vecs);
+    l.team = vecs == 3 ? l.threads : round32((n + vecs - 1) / vecs);
     rows_of_block = l.threads / l.team;
     const int stage = 2 * l.threads * vecs * 8 * static_cast<int>(sizeof(T));
     // two blocks an SM where three stages of each fit

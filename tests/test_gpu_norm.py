@@ -288,3 +288,9 @@ def test_sizes_beyond_32_bits_are_refused(B):
                  lambda: B.nsp_norm_fwd(x[0], w, None, x[0], None, None)):
         with pytest.raises(B.NspError):
             call()
+
+
+@pytest.mark.parametrize("dim", [8320, 11000, 12288, 12296])
+@pytest.mark.parametrize("kind,dtype,w_type,rows", [("layer", "bf16", "f32", 700), ("rms", "bf16", "bf16", 149), ("layer", "f32", "bf16", 300)])
+def test_rows_between_two_and_four_vectors_of_a_thread(B, dim, kind, dtype, w_type, rows):
+    one_case(B, (rows, dim), kind, dtype, w_type)
