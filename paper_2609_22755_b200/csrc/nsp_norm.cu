@@ -1005,29 +1005,31 @@ __global__ void __launch_bounds__(kThreads, 1) norm_bwd_odd_kernel(const NormArg
     if (j < mine.n) *part_w = dw[j], *part_b = db[j];
 }
 
-// dw and db (the second half of the blocks) from the sums of the blocks: 32 columns a block, a warp for every 32nd sum.
+// dw and db (the second half of the blocks) from the sums of the blocks: 32 columns a block, a sum in turn for every warp. 32 warps where
+// two blocks an SM have left theirs, 16 for fewer (148 sums of 16,384 columns: 4 us less than 32), no more than there are sums (one row of
+// 16,384: 16.9 -> 15.0 us both kernels).
 __global__ void __launch_bounds__(1024) norm_grads_kernel(const float* part, int blocks, int dim, float* dw, float* db) {
   __shared__ float sum[32][33];
   grid_wait_predecessor();
   grid_launch_dependents();
   const int half = static_cast<int>(gridDim.x) / 2, which = static_cast<int>(blockIdx.x) >= half;
-  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, c = (blockIdx.x - which * half) * 32 + lane;
+  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5, warps = blockDim.x >> 5, c = (blockIdx.x - which * half) * 32 + lane;
   float* const out = which ? db : dw;
   if (!out) return;
   const float* p = part + static_cast<int64_t>(which) * blocks * dim + c;
   float total = 0.f;
   if (c < dim) {
 #pragma unroll 8
-    for (int i = k; i < blocks; i += 32) total += p[static_cast<int64_t>(i) * dim];
+    for (int i = k; i < blocks; i += warps) total += p[static_cast<int64_t>(i) * dim];
   }
-  sum[k][lane] = total;
-  __syncthreads();
-  if (k == 0 && c < dim) {
+  if (warps > 1) {
+    sum[k][lane] = total;
+    __syncthreads();
+    if (k > 0) return;
     total = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) total += sum[i][lane];
-    out[c] = total;
+    for (int i = 0; i < warps; ++i) total += sum[i][lane];
   }
+  if (c < dim) out[c] = total;
 }
 
 constexpr int kSms = 148;
@@ -1098,8 +1100,8 @@ Launch fwd_launch(int dim, int64_t rows) {
     if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 4, 2);
     else NSP_USE(32, 4, 8, 2);
   }
-  else if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 8, 1);
-  else NSP_USE(32, 4, 16, 1);
+  else if (sizeof(T) == 2 && rows > 2 * kSms) NSP_USE(32, 8, 8, 1);
+  else NSP_USE(32, 4, 16, 1);  // fp32, and few rows (one row of 16,384 bf16: 3.7 us, with half the warps 4.6)
 #undef NSP_USE
   l.blocks = (rows + per_block - 1) / per_block;
   return l;
@@ -1266,6 +1268,7 @@ extern "C" int nsp_norm_bwd(const nsp_rows_t* x, const nsp_rows_t* dy, const voi
   }
   if (!grads) return NSP_OK;
   nsp::count_launches(1);
-  return nsp::launch_chained_if(true, norm_grads_kernel, 2 * ((dim + 31) / 32), 1024, 0, st, static_cast<const float*>(ws), blocks, dim,
+  const int warps = blocks >= 256 ? 32 : blocks >= 16 ? 16 : blocks > 1 ? blocks : 1;
+  return nsp::launch_chained_if(true, norm_grads_kernel, 2 * ((dim + 31) / 32), 32 * warps, 0, st, static_cast<const float*>(ws), blocks, dim,
                                 dweight, dbias) == cudaSuccess ? NSP_OK : NSP_ERR_CUDA;
 }
