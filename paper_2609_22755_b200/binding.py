@@ -739,10 +739,12 @@ def nsp_rope(xs, ys, positions, inv_freq, layout=NSP_ROPE_HALF, magnitude=1.0, i
             _refuse(what, f"x has shape {tuple(shape)}", NSP_ERR_UNSUPPORTED)
         if pos is None:
             at = 0
-        elif pos is not known or tokens != known_tokens:
-            if pos.dtype != _Torch.i64 or pos.shape != (tokens,) or not pos.is_contiguous():
-                _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
-            known, known_tokens, at = pos, tokens, pos.data_ptr()
+        else:
+            if pos is not known or tokens != known_tokens:
+                if pos.dtype != _Torch.i64 or pos.shape != (tokens,) or not pos.is_contiguous():
+                    _refuse(what, "positions must be a contiguous int64 tensor with one entry per token")
+                known, known_tokens, known_at = pos, tokens, pos.data_ptr()
+            at = known_at
         if tokens * heads * head_dim == 0:
             continue
         packed.append(_ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), at, tokens, sx[0], sx[1], sy[0], sy[1], heads, _dtype_of(what, "x", dtype)))
