@@ -503,8 +503,9 @@ __global__ void __launch_bounds__(fwd_threads(kWarps), fwd_blocks(kVecs, kWarps)
 }
 
 // What a thread does with a vector of a row: the sums of t h and t and the parameters' gradients, and dx. A row's constants:
-//     h = x r + shift, shift = -mu r;   dx = r t + x slope + offset, slope = -r^2 c1, offset = -r (c1 shift + c2)
-// with c1 = mean(t h), c2 = mean(t): the products of h are taken apart so that a pair of elements takes three instructions.
+//     h = (x - mu) r;   dx = r t + (x - mu) slope + offset, slope = -r^2 c1, offset = -r c2
+// with c1 = mean(t h), c2 = mean(t): the products of h are taken apart so that a pair of elements takes four instructions. mu is
+// subtracted first, as in the forward pass (x slope + (offset - mu slope) would save one and leave the roundings of mu slope).
 enum : int { kRms = 0, kRmsBias = 1, kLayerBias = 2 };  // whether mean(t) is subtracted and db is summed up
 // Pairs of fp32 in one 64-bit register, as the packed instructions take them.
 struct F2 {
@@ -550,31 +551,31 @@ struct BwdVec {
     }
   };
   __device__ __forceinline__ static F2 pair(const Vec<T, 8>& x, int k) { return F2::of(x.get(2 * k), x.get(2 * k + 1)); }
-  __device__ __forceinline__ static void sums(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 shift, F2& s, F2& c, Params& dw,
+  __device__ __forceinline__ static void sums(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 minus_mu, F2& s, F2& c, Params& dw,
                                               Params& db) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const F2 g = pair(dy, k), u = pair(x, k);
-      const F2 gh = mul(kKind == kLayerBias ? fma(u, r, shift) : mul(u, r), g);
+      const F2 gh = mul(mul(kKind == kLayerBias ? add(u, minus_mu) : u, r), g);
       s = fma(w.v[k], gh, s);
       dw.v[k] = add(dw.v[k], gh);
       if (kKind == kLayerBias) c = fma(w.v[k], g, c);
       if (kKind != kRms) db.v[k] = add(db.v[k], g);
     }
   }
-  __device__ __forceinline__ static void grad(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 slope, F2 offset, char* out, int v,
-                                              bool here = true) {
+  __device__ __forceinline__ static void grad(const Vec<T, 8>& x, const Vec<T, 8>& dy, const Params& w, F2 r, F2 minus_mu, F2 slope, F2 offset, char* out,
+                                              int v, bool here = true) {
     float o[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const F2 u = pair(x, k);
-      const F2 d = fma(mul(pair(dy, k), w.v[k]), r, kKind == kLayerBias ? fma(u, slope, offset) : mul(u, slope));
+      const F2 d = fma(mul(pair(dy, k), w.v[k]), r, kKind == kLayerBias ? fma(add(u, minus_mu), slope, offset) : mul(u, slope));
       o[2 * k] = d.lo(), o[2 * k + 1] = d.hi();
     }
     if (here) Vec<T, 8>::store(out, v, o);
   }
   __device__ __forceinline__ static float slope(float r, float c1) { return -r * r * c1; }
-  __device__ __forceinline__ static float offset(float r, float shift, float c1, float c2) { return -r * fmaf(c1, shift, c2); }
+  __device__ __forceinline__ static float offset(float r, float c2) { return -r * c2; }
 };
 __device__ __forceinline__ F2 both(float x) { return F2::of(x, x); }
 
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
   const int64_t step = static_cast<int64_t>(gridDim.x) * kTeams * kRows;
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * kTeams * kRows; base < a.rows; base += step) {
     Vec<T, 8> x[kRows][kVecs], dy[kRows][kVecs];
-    float r[kRows], shift[kRows];
+    float r[kRows], minus_mu[kRows];
     char* out[kRows];
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
         if (here && lane + j * kLanes < n_vec) x[q][j].load(px, lane + j * kLanes), dy[q][j].load(pg, lane + j * kLanes);
       }
       r[q] = here ? a.rstd[row] : 0.f;
-      shift[q] = kKind == kLayerBias && here ? -a.mean[row] * r[q] : 0.f;
+      minus_mu[q] = kKind == kLayerBias && here ? -a.mean[row] : 0.f;
     }
     float sum[kSums];
 #pragma unroll
@@ -621,7 +622,7 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
       F2 s{0}, c{0};
 #pragma unroll
       for (int j = 0; j < kVecs; ++j)
-        if (lane + j * kLanes < n_vec) B::sums(x[q][j], dy[q][j], w[j], both(r[q]), both(shift[q]), s, c, dw[j], db[j]);
+        if (lane + j * kLanes < n_vec) B::sums(x[q][j], dy[q][j], w[j], both(r[q]), both(minus_mu[q]), s, c, dw[j], db[j]);
       sum[q] = s.sum();
       if (kKind == kLayerBias) sum[kRows + q] = c.sum();
     }
@@ -630,12 +631,12 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
     for (int q = 0; q < kRows; ++q) {
       const float c1 = __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(q), kLanes);
       const float c2 = kKind == kLayerBias ? __shfl_sync(0xffffffffu, mine, sum_at<kSums, kLanes>(kRows + q), kLanes) : 0.f;
-      const float slope = B::slope(r[q], c1), offset = B::offset(r[q], shift[q], c1, c2);
+      const float slope = B::slope(r[q], c1), offset = B::offset(r[q], c2);
       if (out[q]) {
 #pragma unroll
         for (int j = 0; j < kVecs; ++j)
           if (lane + j * kLanes < n_vec)
-            B::grad(x[q][j], dy[q][j], w[j], both(r[q]), both(slope), both(offset), out[q], lane + j * kLanes);
+            B::grad(x[q][j], dy[q][j], w[j], both(r[q]), both(minus_mu[q]), both(slope), both(offset), out[q], lane + j * kLanes);
       }
     }
   }
@@ -757,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
   int turn = 0, stage = 0;
   const float inv_dim = a.inv_dim;
   for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.rows; base += step, turn ^= 1) {
-    const float r = next_r, shift = -next_mu * r;
+    const float r = next_r, minus_mu = -next_mu;
     wait_oldest(stages);
     const char* const from = ring + stage * kStageBytes + threadIdx.x * kVecBytes;
     Vec<T, 8> x[kVecs], dy[kVecs];
@@ -767,7 +768,8 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
     for (int j = 0; j < kVecs; ++j) {
       if (idle(j)) continue;
       read(j);
-      B::sums(x[j], dy[j], weights(j), both(r), both(shift), s, c, dw[j], db[j]);
+      // (a vector that does not exist is centred by a factor of 0, or its zeros would be 0 - mu, times r perhaps not finite)
+      B::sums(x[j], dy[j], weights(j), both(kKind == kLayerBias && !on[j] ? 0.f : r), both(minus_mu), s, c, dw[j], db[j]);
     }
     float sum[kParts];
     sum[0] = s.sum();
@@ -794,13 +796,13 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_long_kernel
       for (int i = 0; i < kParts; ++i) total[i] = __shfl_sync(0xffffffffu, v, i * kWide);
     }
     const float c1 = total[0], c2 = kKind == kLayerBias ? total[kParts - 1] : 0.f;
-    const float slope = B::slope(r, c1), offset = B::offset(r, shift, c1, c2);
+    const float slope = B::slope(r, c1), offset = B::offset(r, c2);
     const bool here = out.r < a.rows;
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
       if (idle(j)) continue;
       if (!kHeld) read(j);
-      B::grad(x[j], dy[j], weights(j), both(r), both(slope), both(offset), out.p[0], tid + j * team_threads, here && on[j]);
+      B::grad(x[j], dy[j], weights(j), both(r), both(minus_mu), both(slope), both(offset), out.p[0], tid + j * team_threads, here && on[j]);
     }
     if (!kHeld) fetch(now);
     out.next();

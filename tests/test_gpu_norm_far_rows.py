@@ -50,3 +50,30 @@ def test_constant_rows_are_centred_to_zero(B, dim, dtype):
     assert torch.equal(y, b.to(x.dtype).expand_as(y))  # 0 w + b
     # 1 / sqrt(eps) with the roundings of 1e-5 to fp32, of the root and of the quotient
     assert bool(((rstd.double() * 1e-5 ** 0.5 - 1).abs() <= 3 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", DIMS)
+def test_gradients_of_constant_rows(B, dim, dtype, eps):
+    """h = 0: such rows add nothing to dweight, and dx = rstd (t - mean(t)), also where mean * rstd leaves fp32 (2^110 * 10^6)."""
+    import torch
+
+    U, dt = 2.0 ** -24, types(dtype)
+    x = torch.cat([constant_rows(dim, dt), torch.full((1, dim), 2.0 ** 110, device="cuda", dtype=dt)])
+    g = torch.Generator("cuda").manual_seed(dim)
+    dy, w = torch.randn(x.shape, generator=g, device="cuda").to(dt), torch.randn(dim, generator=g, device="cuda")
+    mean, rstd = x[:, 0].float().contiguous(), torch.full((len(x),), eps ** -0.5, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    ws = torch.empty(B.nsp_norm_bwd_ws_bytes(len(x), dim), dtype=torch.uint8, device="cuda")
+    B.nsp_norm_bwd(x, dy, w, mean, rstd, dx, dw, db, ws)
+    assert torch.equal(dw, torch.zeros_like(dw))
+    t, r = dy.double() * w.double(), rstd.double()[:, None]
+    c2 = t.mean(-1, keepdim=True)
+    want = r * (t - c2)
+    # t, its difference from the mean and the product with rstd are rounded once each; the mean is a sum of 48 additions one behind the
+    # other at most (32 of a thread, 5 in a warp, 5 over the warps, and products)
+    bound = r * U * (4 * t.abs() + 4 * c2.abs() + 52 * t.abs().mean(-1, keepdim=True))
+    off, half = (dx.double() - want).abs(), torch.finfo(dt).eps / 2
+    assert bool((off <= bound + half * (want.abs() + bound)).all())
+    assert bool(((db.double() - dy.double().sum(0)).abs() <= len(x) * U * dy.double().abs().sum(0)).all())
