@@ -1041,6 +1041,7 @@ __global__ void __launch_bounds__(1024) norm_grads_kernel(const float* part, int
 
 constexpr int kSms = 148;
 constexpr int kMostShared = 227 * 1024;
+constexpr int kStaticShared = 1024;  // no less than the kernels with dynamic shared memory have of their own
 
 // A launch: which kernel, blocks and threads; shared memory, stages and threads of a row of the long rows' kernel.
 struct Launch {
@@ -1167,7 +1168,9 @@ Launch launch_of(bool vectors, int dim, int64_t rows, int dtype, bool layer, boo
 
 cudaError_t launch(const Launch& l, NormArgs& a, cudaStream_t st) {
   if (l.shared > 40 * 1024) {  // with what the kernel has of its own, more than the 48 KB of an ordinary launch
-    const cudaError_t e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.shared);
+    // The same value in every call, whatever this one needs: the attribute is the kernel's, and a smaller one would make the launch of
+    // another thread fail that has just set what it needs.
+    const cudaError_t e = cudaFuncSetAttribute(l.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared - kStaticShared);
     if (e != cudaSuccess) return cudaGetLastError(), e;
   }
   a.stages = l.stages, a.team = l.team;
