@@ -1108,8 +1108,8 @@ Launch fwd_launch(int dim, int64_t rows) {
     if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 4, 2);
     else NSP_USE(32, 4, 8, 2);
   }
-  else if (sizeof(T) == 2 && rows > 2 * kSms) NSP_USE(32, 8, 8, 1);
-  else NSP_USE(32, 4, 16, 1);  // fp32, and few rows (one row of 16,384 bf16: 3.7 us, with half the warps 4.6)
+  else if (sizeof(T) == 4 || rows <= 2 * kSms) NSP_USE(32, 4, 16, 1);  // fp32, and few rows (one row of 16,384 bf16: 3.7 us, with half the warps 4.6)
+  else if constexpr (sizeof(T) == 2) NSP_USE(32, 8, 8, 1);
 #undef NSP_USE
   l.blocks = (rows + per_block - 1) / per_block;
   return l;
