@@ -111,15 +111,21 @@ class NspAttention:
         """The queries and keys that attention reads."""
         return (self.q, self.k) if self.rope is None else (self.q_rot, self.k_rot)
 
-    def forward(self):
+    def _rotate_in(self):
         if self.rope is not None:
             self.rope.rotate(self._rope_in, self._rope_out, self._run_positions, stream=self.stream)
+
+    def forward(self):
+        self._rotate_in()
         q, k = self._qk()
         B.nsp_attn_fwd(self.plan, q, k, self.v, self.o, self.lse, self.scale, stream=self.stream)
 
     def backward(self, recompute=None):
         """recompute: optional uint8 flags per segment (see nsp_recompute_mark): O and LSE of a flagged segment are
-        not read, the backward pass recomputes what it needs of them."""
+        not read, the backward pass recomputes what it needs of them. With ``rope`` the rotated queries and keys are the
+        forward pass's; where there are flags they are made anew, so that q and k are all that a flagged segment needs."""
+        if recompute is not None:
+            self._rotate_in()
         q, k = self._qk()
         if recompute is None:
             B.nsp_attn_bwd(self.plan, q, k, self.v, self.o, self.do, self.lse, self.dq, self.dk, self.dv,
