@@ -312,7 +312,9 @@ int nsp_a2a_scatter_heads(const void* src, void* dst, int64_t tokens, int32_t he
  * The first rot_dim elements of a head are rot_dim / 2 pairs, pair i of NSP_ROPE_HALF the elements (i, rot_dim / 2 + i), of
  * NSP_ROPE_INTERLEAVED (2 i, 2 i + 1). At position p a pair (a, b) becomes (a c - b s, b c + a s) with
  * c = magnitude * cos(p * inv_freq[i]), s = magnitude * sin(p * inv_freq[i]); inverse != 0: with -s, the gradient of that. The
- * other elements pass as they are. fp32 arithmetic, angles exact for any position (64-bit fixed point), one rounding.
+ * other elements pass as they are. fp32 arithmetic, one rounding. Angles are kept in 64-bit fixed point, as parts of a turn: off by at
+ * most 2^-32 of a turn (1.5e-9 radians), and |position| * 2^-63 of one for frequencies of up to 2 pi radians per position, which stays
+ * below a step of fp32 for positions of up to 2^36. A larger frequency loses in proportion to its size.
  *
  * tensors: host array [n_tensors], n_tensors <= NSP_ROPE_MAX_TENSORS, all of them in one launch: for example q and k of a node,
  * or of every node of a chain. A tensor is [tokens, heads, head_dim] with element strides between tokens and heads

@@ -4,7 +4,9 @@ forward + backward of the local attention compute phase through the C ABI.
 Only marshalling lives here. ``step_device`` runs on tensors already resident on the GPU; ``step_host`` is the
 end-to-end call (nsp_attn_step_host): Q, K, V, dO come from (pinned) host tensors and O, LSE, dQ, dK, dV go back to
 host tensors; the library makes the copies on a second stream under the kernels where the data dependencies allow.
-With ``rope`` the queries and keys are rotated by their positions on the way in and the gradients dQ and dK on the way back.
+With ``rope`` the queries and keys are rotated by their positions on the way in and the gradients dQ and dK on the way back, in
+place, as the backward pass has left them: gradients in bf16 are then rounded a second time (``dq_dtype`` and ``dkv_dtype`` "f32"
+have one rounding, to fp32).
 """
 from __future__ import annotations
 

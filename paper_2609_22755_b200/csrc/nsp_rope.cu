@@ -7,7 +7,9 @@
 // The angle. p f reaches 10^5 radians and more, where 32 bits leave two or three digits of the angle. A frequency is therefore
 // kept as a fraction of a turn in 64-bit fixed point, F = 2^64 frac(f / 2 pi): p F modulo 2^64 is the exact fractional
 // turn of p F (an integer product drops whole turns by itself). Its upper 32 bits give the quarter turn and, as a signed number,
-// the rest within an eighth; the error is p * 2^-63 of a turn, for any p a batch can have below the rounding of the cosine.
+// the rest within an eighth; the lower ones are cut off. The error is 2^-32 of a turn from that cut, and |p| times the frequency's own: F has
+// that of the product f / 2 pi in 64 bits and of the cut behind it, together below 2^-63 of a turn for |f| <= 2 pi (frequencies of several
+// turns a position lose as many more bits as their whole turns take). Both are below the rounding of the cosine for |p| <= 2^36.
 //
 // Work. A thread owns V pairs of a head (one 16-byte load for each half of them in bf16) of up to 16 neighbouring heads of one
 // token, or of all heads of q and of k where they are no more (a chain's upper nodes: 4 and 1): the sines and cosines are computed
@@ -108,7 +110,7 @@ struct Raw {
 
 // m cos and m sin of a turn in 64-bit fixed point (sin_m: m or -m). The rest of the angle behind its quarter turn, f in [-pi/4, pi/4],
 // goes through polynomials in f^2 fitted for the smallest relative error by reweighted least squares (sine 3.8e-9, cosine 1.2e-10);
-// in fp32 both are within 1.7 * 2^-24. A third of the instructions of a general sincospi, which has to find the quarter turn of a
+// in fp32 both are within 1.7 * 2^-24 of those of f. A third of the instructions of a general sincospi, which has to find the quarter turn of a
 // float.
 __device__ __forceinline__ void sincos_turn(uint64_t turn, float m, float sin_m, float& c, float& s) {
   const uint32_t top = static_cast<uint32_t>(turn >> 32), quarter = (top + 0x20000000u) >> 30;

@@ -11,7 +11,8 @@ reverse exchange (which also adds the partial dK / dV of a KV head that several 
 
 Rotary positions are applied on the token slices, where every KV head is there once (behind the exchange a head that several GPUs
 share would be rotated by each of them): ``rope`` of the prologue rotates on the way in, of the epilogue the gradients on the way
-back; ``NodeLayout.positions`` are those of a GPU's slices.
+back, in place behind the sum over GPUs: gradients in bf16 are rounded a second time. ``NodeLayout.positions`` are those of a GPU's
+slices.
 
 The layout steps run in the library's CUDA kernels (``CudaLayoutOps``); the exchange goes through
 ``torch.distributed`` (NCCL between GPUs). ``phase_streams`` runs the communication of the next node on its own stream

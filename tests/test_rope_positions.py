@@ -46,3 +46,27 @@ def test_one_call_is_as_many_single_ones(order):
     for x, w, p in zip(xs, want, pos):
         B.nsp_rope(x, w, p, freq)
     assert all(torch.equal(y, w) for y, w in zip(ys, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", [0, 1])
+def test_angles_are_as_good_as_stated(layout):
+    """Cosines and sines themselves, of pairs (1, 0), at positions of up to 2^36 and frequencies of up to a turn a position, and some of several
+    turns: the angle within 2 pi (2^-32 + |p| 2^-63 max(1, |f| / 2 pi)), the polynomials within 1.7 * 2^-24, their factor and the sum
+    of the two products 2^-24 each."""
+    from fractions import Fraction
+
+    pi = Fraction(3141592653589793238462643383279502884197169399375105820974945, 10 ** 60)
+    rng = np.random.default_rng(4)
+    pos = np.concatenate([[0, 1, -1, 2, 2 ** 36, -2 ** 36], (2.0 ** rng.uniform(0, 36, 200)).astype(np.int64) * rng.choice([-1, 1], 200)])
+    freq = np.concatenate([rng.uniform(-2 * np.pi, 2 * np.pi, 20), [1.0, 1e-6, 3.14159, 6.28, 100.0, -1e4], 1e6 ** -rng.uniform(0, 1, 6)])
+    x = torch.zeros(len(pos), 1, 2 * len(freq), device="cuda")
+    first = (slice(0, len(freq)), slice(len(freq), None)) if layout == 0 else (slice(0, None, 2), slice(1, None, 2))
+    x[..., first[0]] = 1.0
+    y = torch.empty_like(x)
+    B.nsp_rope(x, y, torch.as_tensor(pos).cuda(), freq, layout=layout)
+    turns = np.array([[float((int(p) * Fraction(float(f)) / (2 * pi)) % 1) for f in freq] for p in pos])
+    bound = 2 * np.pi * (2.0 ** -32 + np.abs(pos)[:, None] * 2.0 ** -63 * np.maximum(1, np.abs(freq) / (2 * np.pi))) + 3.7 * 2.0 ** -24
+    for at, exact in ((first[0], np.cos), (first[1], np.sin)):
+        off = np.abs(y[:, 0, at].double().cpu().numpy() - exact(2 * np.pi * turns))
+        assert (off <= bound).all(), (off / bound).max()
