@@ -15,7 +15,7 @@
 // which bounds its columns to 16 or 32; long rows come through shared memory some rows ahead by asynchronous copies (each thread
 // copies and reads its own vectors: no barrier), and a row's sums are exchanged at one barrier. The blocks'
 // gradients go to the workspace and a second kernel adds them in their order: the same bits in every run.
-// Rows whose addresses do not allow vectors go element by element through kernels of their own: short ones by lanes of a warp
+// Rows whose addresses do not allow vectors (14-44 % of the copy rate in bf16) go element by element through kernels of their own: short ones by lanes of a warp
 // (norm_*_element_kernel), long ones by a block (norm_*_odd_kernel), whose rows come through shared memory in the 16-byte pieces they
 // lie in, some rows ahead. (16,384 rows of 2,051 bf16 by loads of single elements, a row ahead in registers: 102 us there, 233 back; so 75 and 110.)
 #include <cmath>
@@ -669,7 +669,9 @@ __global__ void __launch_bounds__(256) norm_bwd_short_kernel(const NormArgs a) {
 // barrier a row). One row at a time: two at one barrier take more registers than two blocks an SM have (32,768 x 4,096: 141 us, with
 // two rows 276, and 512 threads of one vector 298). Rows of more than 8,192 elements take four vectors a thread: halves of a row in the CTAs
 // of a cluster, its barrier hidden behind the next row's sums, gain with two sums a row and lose with one (4,096 x 16,384: layer norm 143 us,
-// halves 123; RMS 110 and 111; 4,096 x 12,288 RMS 96 and 104; 8,192 x 8,320 193 and 205).
+// halves 123; RMS 110 and 111; 4,096 x 12,288 RMS 96 and 104; 8,192 x 8,320 193 and 205). The faster form for long layer norms is left for a
+// kernel of its own. These figures, and those in the kernel, are of the order of products that BwdVec names as the faster one: 2-3 % are to
+// be added for layer norm.
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, uint32_t bytes) {  // 16, or none: zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
